@@ -411,6 +411,50 @@ int occult_expert_ffn_backward_weights_ws(const occult_cfg_t* cfg, const occult_
                                           float* dw_up, float* dw_down, int accumulate, void* ws, size_t ws_bytes,
                                           occult_stream_t stream);
 
+/* The block around the layer: the norms before and after it, fused with its gate, its residual scale and the residual sum.  With
+ * y [T][d] the block's output (occult_combine's y) and x [T][d] the residual stream in front of the block,
+ *   out[t] = x_scale * x[t] + y_scale * gate(t) * N_post(y[t])          the stream behind the block
+ *   h[t]   = N_pre(out[t])                                              what the next block reads
+ * in one pass.  N(v) = (v - mu) / sqrt(mean((v - mu)^2) + eps) * (weight + weight_offset) + bias with mu = 0 (OCCULT_NORM_RMS) or
+ * the row's mean (OCCULT_NORM_LAYER); OCCULT_NORM_NONE leaves the row as it is (post: N_post(y) = y; pre: no h).  Without y the
+ * call is the pre norm alone, h = N_pre(x), and out is not written.  N_pre reads out as rounded to cfg.dtype.  All arithmetic is
+ * f32; a token's results do not depend on T.  Squares of a row are summed in f32: rows whose mean square exceeds
+ * the f32 range are outside of what the call is for.
+ *   weights, bias [d], cfg.dtype, device ptrs, each NULL = factor 1 (weight_offset is then not added) and summand 0;
+ *   gate in cfg.dtype: OCCULT_GATE_CHANNEL [d], OCCULT_GATE_TOKEN [T], OCCULT_GATE_ELEMENT [T][d], OCCULT_GATE_NONE = 1 (NULL).
+ * cfg gives T, d and dtype (its other fields only have to be valid); a row is at most 32768 bytes long.  out may be x or y, and h may
+ * be x or y, but not each other; buffers that overlap in another way are not for this call.
+ *
+ * occult_block_norm_backward: from dout [T][d], the gradient of out from where it is read beside h (NULL = none; needed without a pre
+ * norm), dh [T][d], the gradient of h, and y and out as the forward pass read and wrote them (for the pre norm alone: out = x, dy = NULL):
+ *   D = dout + N_pre'(dh);   dx = x_scale * D;   dy = N_post'(y_scale * gate * D);   gate gradient = y_scale * N_post(y) * D
+ * dx, dy [T][d] in cfg.dtype, one of them may be NULL (dy: then no gradient of post norm or gate either); y may be NULL where there
+ * is neither post norm nor gate.  grads: each NULL or the gradient of that parameter, f32 [d], summed over tokens
+ * (accumulate = 1: added to what is there); gate: CHANNEL f32 [d] likewise, TOKEN f32 [T] and ELEMENT [T][d] in cfg.dtype written
+ * per token whatever accumulate is.  The sums over tokens go through ws (device ptr, 16-byte aligned,
+ * >= occult_block_norm_backward_ws_bytes() bytes, contents not kept) in a fixed order, without atomics.  T == 0 writes zeros to the sums /
+ * adds nothing.  dx may be dout, dh or out, and dy may be y, dout, dh or out, but not each other. */
+enum { OCCULT_NORM_NONE = 0, OCCULT_NORM_RMS = 1, OCCULT_NORM_LAYER = 2 };
+enum { OCCULT_GATE_NONE = 0, OCCULT_GATE_CHANNEL = 1, OCCULT_GATE_TOKEN = 2, OCCULT_GATE_ELEMENT = 3 };
+typedef struct occult_block_norm {
+  int32_t post_kind, pre_kind;   /* OCCULT_NORM_*                                    */
+  int32_t gate_kind;             /* OCCULT_GATE_*                                    */
+  float x_scale, y_scale;        /* finite                                           */
+  float post_eps, pre_eps;       /* positive where the norm is there                 */
+  float weight_offset;           /* 0, or 1 for weights stored as differences from 1 */
+  const void *post_weight, *post_bias, *pre_weight, *pre_bias, *gate;
+} occult_block_norm_t;
+typedef struct occult_block_norm_grads {
+  float *post_weight, *post_bias, *pre_weight, *pre_bias;
+  void* gate;
+} occult_block_norm_grads_t;
+int occult_block_norm(const occult_cfg_t* cfg, const occult_block_norm_t* norm, const void* x, const void* y, void* out, void* h,
+                      occult_stream_t stream);
+int occult_block_norm_backward_ws_bytes(const occult_cfg_t* cfg, const occult_block_norm_t* norm, size_t* ws_bytes);
+int occult_block_norm_backward(const occult_cfg_t* cfg, const occult_block_norm_t* norm, const void* y, const void* out,
+                               const void* dout, const void* dh, void* dx, void* dy, const occult_block_norm_grads_t* grads,
+                               int accumulate, void* ws, size_t ws_bytes, occult_stream_t stream);
+
 /* Gradient of the routing weights with respect to the router scores (paper Eq. 1: Softmax over
  * all E experts, the values at the selected experts, divided by their sum if cfg.renorm; the
  * selection is piecewise constant and has no gradient).  logits [T][E] f32, ids [T][k] as returned

@@ -17,6 +17,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "liboccult.so")
 
 OCCULT_F32, OCCULT_BF16 = 0, 1
+OCCULT_NORM_NONE, OCCULT_NORM_RMS, OCCULT_NORM_LAYER = 0, 1, 2
+OCCULT_GATE_NONE, OCCULT_GATE_CHANNEL, OCCULT_GATE_TOKEN, OCCULT_GATE_ELEMENT = 0, 1, 2, 3
 
 EXPORTS = [
     "occult_version", "occult_last_error", "occult_plan_sizes", "occult_plan_bind", "occult_route",
@@ -28,6 +30,7 @@ EXPORTS = [
     "occult_pack_weights_bytes", "occult_pack_weights", "occult_expert_ffn_packed", "occult_expert_ffn_train",
     "occult_collaboration_stats", "occult_plan_static", "occult_combine_atomic",
     "occult_expert_ffn_backward_weights_ws_bytes", "occult_expert_ffn_backward_weights_ws", "occult_forward",
+    "occult_block_norm", "occult_block_norm_backward", "occult_block_norm_backward_ws_bytes",
 ]
 
 
@@ -59,6 +62,16 @@ class occult_forward_buffers_t(Structure):
     _fields_ = [(n, c_void_p) for n in ("ids", "w", "plan_ws", "sfd_x", "epd_h", "epd_y", "h_shared", "y_shared", "ffn_ws",
                                         "epd_gu", "gu_shared", "sfd_y", "y")] + [
                 ("plan_ws_bytes", c_size_t), ("ffn_ws_bytes", c_size_t)]
+
+
+class occult_block_norm_t(Structure):
+    _fields_ = ([(n, c_int32) for n in ("post_kind", "pre_kind", "gate_kind")] +
+                [(n, c_float) for n in ("x_scale", "y_scale", "post_eps", "pre_eps", "weight_offset")] +
+                [(n, c_void_p) for n in ("post_weight", "post_bias", "pre_weight", "pre_bias", "gate")])
+
+
+class occult_block_norm_grads_t(Structure):
+    _fields_ = [(n, c_void_p) for n in ("post_weight", "post_bias", "pre_weight", "pre_bias", "gate")]
 
 
 class occult_stats_t(Structure):
@@ -125,6 +138,11 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.occult_placement_greedy.argtypes = [c_void_p, c_int32, c_int32, c_void_p, c_void_p]
     lib.occult_collaboration_stats.argtypes = [c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p]
     lib.occult_plan_stats.argtypes = [cfgp, planp, POINTER(occult_stats_t), c_void_p]
+    normp = POINTER(occult_block_norm_t)
+    lib.occult_block_norm.argtypes = [cfgp, normp] + [c_void_p] * 5
+    lib.occult_block_norm_backward_ws_bytes.argtypes = [cfgp, normp, POINTER(c_size_t)]
+    lib.occult_block_norm_backward.argtypes = ([cfgp, normp] + [c_void_p] * 6 + [POINTER(occult_block_norm_grads_t), c_int, c_void_p,
+                                               c_size_t, c_void_p])
     for name in EXPORTS:
         if name not in ("occult_version", "occult_last_error"):
             getattr(lib, name).restype = c_int
@@ -412,3 +430,29 @@ def occult_plan_stats(cfg, plan, stream=None) -> occult_stats_t:
     _check(load_library().occult_plan_stats(ctypes.byref(cfg), ctypes.byref(plan), ctypes.byref(st),
                                             _stream(stream)))
     return st
+
+
+def make_block_norm(post_kind, pre_kind, gate_kind, x_scale=1.0, y_scale=1.0, post_eps=1e-6, pre_eps=1e-6, weight_offset=0.0,
+                    post_weight=None, post_bias=None, pre_weight=None, pre_bias=None, gate=None) -> occult_block_norm_t:
+    """Kinds: OCCULT_NORM_*, OCCULT_GATE_*.  The tensors are the caller's to keep alive."""
+    return occult_block_norm_t(post_kind, pre_kind, gate_kind, x_scale, y_scale, post_eps, pre_eps, weight_offset, _ptr(post_weight),
+                               _ptr(post_bias), _ptr(pre_weight), _ptr(pre_bias), _ptr(gate))
+
+
+def occult_block_norm(cfg, norm: occult_block_norm_t, x, y, out, h, stream=None) -> None:
+    _check(load_library().occult_block_norm(ctypes.byref(cfg), ctypes.byref(norm), _ptr(x), _ptr(y), _ptr(out), _ptr(h),
+                                            _stream(stream)))
+
+
+def occult_block_norm_backward_ws_bytes(cfg, norm: occult_block_norm_t) -> int:
+    n = c_size_t(0)
+    _check(load_library().occult_block_norm_backward_ws_bytes(ctypes.byref(cfg), ctypes.byref(norm), ctypes.byref(n)))
+    return int(n.value)
+
+
+def occult_block_norm_backward(cfg, norm: occult_block_norm_t, y, out, dout, dh, dx, dy, dpost_weight=None, dpost_bias=None,
+                               dpre_weight=None, dpre_bias=None, dgate=None, accumulate=False, ws=None, stream=None) -> None:
+    grads = occult_block_norm_grads_t(_ptr(dpost_weight), _ptr(dpost_bias), _ptr(dpre_weight), _ptr(dpre_bias), _ptr(dgate))
+    _check(load_library().occult_block_norm_backward(
+        ctypes.byref(cfg), ctypes.byref(norm), _ptr(y), _ptr(out), _ptr(dout), _ptr(dh), _ptr(dx), _ptr(dy), ctypes.byref(grads),
+        int(bool(accumulate)), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)))

@@ -1,0 +1,705 @@
+// occult_block_norm and its backward pass: the norms around a block, fused with its gate, its residual scale and the residual sum.
+//
+//   forward   out = x_scale * x + y_scale * gate * N_post(y);   h = N_pre(out)
+//   backward  D = dout + N_pre'(dh);   dx = x_scale * D;   dz = y_scale * gate * D;   dy = N_post'(dz);   dgate = y_scale * z * D
+//   with N(v) = vh * w + b, vh = (v - mu) * r, r = 1 / sqrt(mean((v - mu)^2) + eps), mu = 0 (RMS) or mean(v) (LAYER), and
+//   N'(g) = r * (q - vh * mean(q * vh) - [LAYER] mean(q)), q = g * w.
+//
+// Bound by HBM: a handful of operations per element.  Every row is read once and written once: the lanes that share a row keep it in
+// registers from the first sum to the last store, so the row statistics cost no second read, and the backward pass
+// recomputes them from the rows that it reads anyway instead of reading kept ones.  A row of up to 64 vectors of 16 bytes
+// belongs to the smallest power of two of lanes that holds it (a wave then works on several rows), a longer one to one wave with several
+// vectors per lane, and still longer ones to several waves, which exchange their sums through LDS.  All sums are f32; which lanes add
+// what depends on the row length alone, so a token's results do not depend on the batch around it.
+#include "common.h"
+
+#include <math.h>
+
+namespace occult {
+
+namespace norm {
+
+constexpr int kMaxRowBytes = 32768;
+constexpr int kColSums = 5;          // post weight, post bias, pre weight, pre bias, channel gate
+constexpr int kBackwardBlocks = 512; // workgroups of the backward pass that keep column sums, at most
+
+struct Args {
+  const void *x, *y, *gate, *post_w, *post_b, *pre_w, *pre_b;
+  void *out, *h;
+  int T, row_vecs, lanes;            // lanes: lanes of a row where a wave holds several rows
+  int post, pre, gate_kind;
+  float x_scale, y_scale, post_eps, pre_eps, offset, inv_d;
+};
+
+struct BackwardArgs {
+  const void *y, *out, *dout, *dh, *gate, *post_w, *post_b, *pre_w;
+  void *dx, *dy, *dgate;             // dgate: per token (f32) or per element (rows); a channel gate's goes through ws
+  float* ws;                         // [workgroup][column sum][d]
+  int T, row_vecs, lanes;
+  int post, pre, gate_kind, sums;    // sums: bit i = column sum i is wanted
+  float x_scale, y_scale, post_eps, pre_eps, offset, inv_d;
+};
+
+constexpr int block_waves(int W) { return W <= 4 ? 4 : W; }
+
+// Which lanes hold which rows.  V vectors per lane, W waves per row; workgroups of 4 waves, or of W.
+template <int V, int W>
+struct Place {
+  static constexpr int kWaves = block_waves(W);
+  int row, lane, stride;             // row inside the workgroup, lane inside the row, lanes of the row
+  __device__ Place(int lanes) {
+    const int wave = threadIdx.x >> 6, l = threadIdx.x & 63;
+    if constexpr (W == 1) {
+      row = wave * (64 / lanes) + l / lanes;
+      lane = l & (lanes - 1);
+      stride = lanes;
+    } else {
+      row = wave / W;
+      lane = (wave % W) * 64 + l;
+      stride = 64 * W;
+    }
+  }
+  __device__ static int rows_per_block(int lanes) { return W == 1 ? kWaves * (64 / lanes) : kWaves / W; }
+};
+
+// The sums of N values over the lanes of a row, in every lane.  `slot`: alternates between two LDS areas, so that one barrier per
+// exchange is enough.
+template <int W, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], int lanes, int& slot) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    if (W > 1 || o < lanes) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) v[n] += __shfl_xor(v[n], o, 64);
+    }
+  }
+  if constexpr (W > 1) {
+    constexpr int kWaves = block_waves(W);
+    __shared__ float s_sum[2][N][kWaves];
+    const int wave = threadIdx.x >> 6, first = wave / W * W;
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) s_sum[slot][n][wave] = v[n];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      float s = s_sum[slot][n][first];
+#pragma unroll
+      for (int w = 1; w < W; ++w) s += s_sum[slot][n][first + w];
+      v[n] = s;
+    }
+    slot ^= 1;
+  }
+}
+
+// A lane's vectors of a row as loaded; vectors past the row's end are zero.
+template <bool BF16, int V>
+struct RowRegs {
+  using R = Row<BF16>;
+  typename R::Raw raw[V];
+  __device__ void load(const void* base, size_t t, int row_vecs, int lane, int stride, bool valid) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int c = lane + i * stride;
+      raw[i] = typename R::Raw{};
+      if (valid && c < row_vecs) raw[i] = R::load_raw(base, t, row_vecs, c);
+    }
+  }
+  // one value per channel, read by every workgroup: kept in the caches
+  __device__ void load_channels(const void* base, int row_vecs, int lane, int stride) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int c = lane + i * stride;
+      raw[i] = typename R::Raw{};
+      if (base && c < row_vecs) raw[i] = static_cast<const typename R::Raw*>(base)[c];
+    }
+  }
+  // Makes the compiler take the values for new ones: what is kept across rows stays as loaded, in half the registers of its floats.
+  __device__ void keep_raw() {
+#pragma unroll
+    for (int i = 0; i < V; ++i) asm volatile("" : "+v"(raw[i]));
+  }
+  __device__ void unpack(int i, float* v) const { R::unpack(raw[i], v); }
+};
+
+template <bool BF16>
+__device__ __forceinline__ float load_scalar(const void* base, size_t t) {
+  if constexpr (BF16) return __uint_as_float((unsigned)static_cast<const uint16_t*>(base)[t] << 16);
+  else return static_cast<const float*>(base)[t];
+}
+
+// factor of a norm's weight: 1 where there is none
+template <int NE>
+__device__ __forceinline__ void weight_of(bool has, float offset, float* w) {
+#pragma unroll
+  for (int e = 0; e < NE; ++e) w[e] = has ? w[e] + offset : 1.0f;
+}
+
+template <bool BF16, int V, int W>
+__global__ __launch_bounds__(64 * block_waves(W)) void block_norm_kernel(const Args a) {
+  using R = Row<BF16>;
+  constexpr int NE = R::kElems;
+  const Place<V, W> p(a.lanes);
+  const int rows = Place<V, W>::rows_per_block(a.lanes);
+  int slot = 0;
+
+  RowRegs<BF16, V> post_w, post_b, pre_w, pre_b, cgate;
+  post_w.load_channels(a.post_w, a.row_vecs, p.lane, p.stride);
+  post_b.load_channels(a.post_b, a.row_vecs, p.lane, p.stride);
+  pre_w.load_channels(a.pre_w, a.row_vecs, p.lane, p.stride);
+  pre_b.load_channels(a.pre_b, a.row_vecs, p.lane, p.stride);
+  cgate.load_channels(a.gate_kind == OCCULT_GATE_CHANNEL ? a.gate : nullptr, a.row_vecs, p.lane, p.stride);
+
+  // one pass = one row per group of lanes; uniform over the workgroup, which meets in row_sums
+  for (long long t0 = (long long)blockIdx.x * rows; t0 < a.T; t0 += (long long)gridDim.x * rows) {
+    const bool valid = t0 + p.row < a.T;
+    const size_t t = valid ? t0 + p.row : 0;
+    post_w.keep_raw();
+    post_b.keep_raw();
+    pre_w.keep_raw();
+    pre_b.keep_raw();
+    cgate.keep_raw();
+    RowRegs<BF16, V> xr, yr;
+    xr.load(a.x, t, a.row_vecs, p.lane, p.stride, valid);
+    float s[V][NE];   // the residual stream
+#pragma unroll
+    for (int i = 0; i < V; ++i) xr.unpack(i, s[i]);
+    if (a.y) {
+      yr.load(a.y, t, a.row_vecs, p.lane, p.stride, valid);
+      RowRegs<BF16, V> gr;
+      if (a.gate_kind == OCCULT_GATE_ELEMENT) gr.load(a.gate, t, a.row_vecs, p.lane, p.stride, valid);
+      float token_gate = 1.0f;
+      if (a.gate_kind == OCCULT_GATE_TOKEN) token_gate = load_scalar<BF16>(a.gate, t);
+      float z[V][NE];
+#pragma unroll
+      for (int i = 0; i < V; ++i) yr.unpack(i, z[i]);
+      if (a.post) {
+        float mu = 0.0f;
+        if (a.post == OCCULT_NORM_LAYER) {
+          float sum[1] = {0.0f};
+#pragma unroll
+          for (int i = 0; i < V; ++i)
+#pragma unroll
+            for (int e = 0; e < NE; ++e) sum[0] += z[i][e];
+          row_sums<W>(sum, a.lanes, slot);
+          mu = sum[0] * a.inv_d;
+        }
+        float sq[1] = {0.0f};
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const bool in = p.lane + i * p.stride < a.row_vecs;
+#pragma unroll
+          for (int e = 0; e < NE; ++e) {
+            z[i][e] = in ? z[i][e] - mu : 0.0f;
+            sq[0] = fmaf(z[i][e], z[i][e], sq[0]);
+          }
+        }
+        row_sums<W>(sq, a.lanes, slot);
+        const float r = 1.0f / sqrtf(fmaf(sq[0], a.inv_d, a.post_eps));
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          float w[NE], b[NE];
+          post_w.unpack(i, w);
+          post_b.unpack(i, b);
+          weight_of<NE>(a.post_w != nullptr, a.offset, w);
+#pragma unroll
+          for (int e = 0; e < NE; ++e) z[i][e] = fmaf(z[i][e] * r, w[e], b[e]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int c = p.lane + i * p.stride;
+        float g[NE];
+        if (a.gate_kind == OCCULT_GATE_CHANNEL) cgate.unpack(i, g);
+        else if (a.gate_kind == OCCULT_GATE_ELEMENT) gr.unpack(i, g);
+        else
+#pragma unroll
+          for (int e = 0; e < NE; ++e) g[e] = token_gate;
+#pragma unroll
+        for (int e = 0; e < NE; ++e) s[i][e] = fmaf(a.y_scale * g[e], z[i][e], a.x_scale * s[i][e]);
+        // rounds s to what is stored: the next norm is taken of the values that the backward pass, and the next block, will read
+        if (valid && c < a.row_vecs) R::store_round(a.out, t, a.row_vecs, c, s[i]);
+      }
+    }
+    if (a.pre) {
+      float mu = 0.0f;
+      if (a.pre == OCCULT_NORM_LAYER) {
+        float sum[1] = {0.0f};
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const bool in = p.lane + i * p.stride < a.row_vecs;
+#pragma unroll
+          for (int e = 0; e < NE; ++e) sum[0] += in ? s[i][e] : 0.0f;
+        }
+        row_sums<W>(sum, a.lanes, slot);
+        mu = sum[0] * a.inv_d;
+      }
+      float sq[1] = {0.0f};
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const bool in = p.lane + i * p.stride < a.row_vecs;
+#pragma unroll
+        for (int e = 0; e < NE; ++e) {
+          s[i][e] = in ? s[i][e] - mu : 0.0f;
+          sq[0] = fmaf(s[i][e], s[i][e], sq[0]);
+        }
+      }
+      row_sums<W>(sq, a.lanes, slot);
+      const float r = 1.0f / sqrtf(fmaf(sq[0], a.inv_d, a.pre_eps));
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int c = p.lane + i * p.stride;
+        float w[NE], b[NE];
+        pre_w.unpack(i, w);
+        pre_b.unpack(i, b);
+        weight_of<NE>(a.pre_w != nullptr, a.offset, w);
+#pragma unroll
+        for (int e = 0; e < NE; ++e) s[i][e] = fmaf(s[i][e] * r, w[e], b[e]);
+        if (valid && c < a.row_vecs) R::store_round(a.h, t, a.row_vecs, c, s[i]);
+      }
+    }
+  }
+}
+
+// Gradients of what is summed over tokens (weights, biases, a channel gate): every lane adds its columns' contributions over the rows of
+// its workgroup in registers, the workgroup's row groups are added through LDS in their order, and the workgroups' sums go to ws, where
+// column_sums_kernel adds them in order: no atomics, the same bits every time.
+template <bool BF16, int V, int W, bool LAYER>
+__global__ __launch_bounds__(64 * block_waves(W)) void block_norm_backward_kernel(const BackwardArgs a) {
+  using R = Row<BF16>;
+  constexpr int NE = R::kElems;
+  // without a mean-subtracting norm or a bias there are three column sums: weights and gate
+  constexpr int NS = LAYER ? kColSums : 3;
+  constexpr int kPostW = 0, kPreW = 1, kGate = 2, kPostB = LAYER ? 3 : 0, kPreB = LAYER ? 4 : 0;
+  const Place<V, W> p(a.lanes);
+  const int rows = Place<V, W>::rows_per_block(a.lanes);
+  int slot = 0;
+
+  RowRegs<BF16, V> post_w, post_b, pre_w, cgate;
+  post_w.load_channels(a.post_w, a.row_vecs, p.lane, p.stride);
+  post_b.load_channels(a.post_b, a.row_vecs, p.lane, p.stride);
+  pre_w.load_channels(a.pre_w, a.row_vecs, p.lane, p.stride);
+  cgate.load_channels(a.gate_kind == OCCULT_GATE_CHANNEL ? a.gate : nullptr, a.row_vecs, p.lane, p.stride);
+  const bool need_y = a.dy && (a.post || a.gate_kind);
+
+  float col[NS][V][NE];
+#pragma unroll
+  for (int n = 0; n < NS; ++n)
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+#pragma unroll
+      for (int e = 0; e < NE; ++e) col[n][i][e] = 0.0f;
+
+  for (long long t0 = (long long)blockIdx.x * rows; t0 < a.T; t0 += (long long)gridDim.x * rows) {
+    const bool valid = t0 + p.row < a.T;
+    const size_t t = valid ? t0 + p.row : 0;
+    post_w.keep_raw();
+    post_b.keep_raw();
+    pre_w.keep_raw();
+    cgate.keep_raw();
+    RowRegs<BF16, V> yr, outr, doutr, dhr, gr;
+    doutr.load(a.dout, t, a.row_vecs, p.lane, p.stride, valid && a.dout);
+    outr.load(a.out, t, a.row_vecs, p.lane, p.stride, valid && a.pre);
+    dhr.load(a.dh, t, a.row_vecs, p.lane, p.stride, valid && a.pre);
+    yr.load(a.y, t, a.row_vecs, p.lane, p.stride, valid && need_y);
+    gr.load(a.gate, t, a.row_vecs, p.lane, p.stride, valid && a.gate_kind == OCCULT_GATE_ELEMENT);
+    float token_gate = 1.0f;
+    if (a.gate_kind == OCCULT_GATE_TOKEN) token_gate = load_scalar<BF16>(a.gate, t);
+
+    float D[V][NE], o[V][NE], y[V][NE];   // gradient of the stream, the stream and y (less their means)
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      doutr.unpack(i, D[i]);
+      outr.unpack(i, o[i]);
+      yr.unpack(i, y[i]);
+    }
+    if constexpr (LAYER) {
+      float mean[2] = {0.0f, 0.0f};
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+#pragma unroll
+        for (int e = 0; e < NE; ++e) {
+          mean[0] += o[i][e];
+          mean[1] += y[i][e];
+        }
+      row_sums<W>(mean, a.lanes, slot);
+      const float mo = a.pre == OCCULT_NORM_LAYER ? mean[0] * a.inv_d : 0.0f;
+      const float my = a.post == OCCULT_NORM_LAYER ? mean[1] * a.inv_d : 0.0f;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const bool in = p.lane + i * p.stride < a.row_vecs;
+#pragma unroll
+        for (int e = 0; e < NE; ++e) {
+          o[i][e] = in ? o[i][e] - mo : 0.0f;
+          y[i][e] = in ? y[i][e] - my : 0.0f;
+        }
+      }
+    }
+    // squares of both rows, and the two sums of the pre norm's gradient, in one exchange
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      float w[NE], g[NE];
+      pre_w.unpack(i, w);
+      dhr.unpack(i, g);
+      weight_of<NE>(a.pre_w != nullptr, a.offset, w);
+#pragma unroll
+      for (int e = 0; e < NE; ++e) {
+        s[0] = fmaf(o[i][e], o[i][e], s[0]);
+        s[1] = fmaf(y[i][e], y[i][e], s[1]);
+        s[2] = fmaf(g[e] * w[e], o[i][e], s[2]);
+        if (LAYER) s[3] = fmaf(g[e], w[e], s[3]);
+      }
+    }
+    row_sums<W>(s, a.lanes, slot);
+    if (a.pre) {
+      const float r = 1.0f / sqrtf(fmaf(s[0], a.inv_d, a.pre_eps));
+      const float m2 = s[2] * r * a.inv_d, m1 = LAYER && a.pre == OCCULT_NORM_LAYER ? s[3] * a.inv_d : 0.0f;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        float w[NE], g[NE];
+        pre_w.unpack(i, w);
+        dhr.unpack(i, g);
+        weight_of<NE>(a.pre_w != nullptr, a.offset, w);
+#pragma unroll
+        for (int e = 0; e < NE; ++e) {
+          const float hat = o[i][e] * r;
+          D[i][e] = fmaf(r, fmaf(-hat, m2, fmaf(g[e], w[e], -m1)), D[i][e]);
+          col[kPreW][i][e] = fmaf(g[e], hat, col[kPreW][i][e]);
+          if constexpr (LAYER) col[kPreB][i][e] += g[e];
+        }
+      }
+    }
+    if (a.dx) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int c = p.lane + i * p.stride;
+        float v[NE];
+#pragma unroll
+        for (int e = 0; e < NE; ++e) v[e] = a.x_scale * D[i][e];
+        if (valid && c < a.row_vecs) R::store_round(a.dx, t, a.row_vecs, c, v);
+      }
+    }
+    if (!a.dy) continue;   // uniform over the grid
+    const float r = a.post ? 1.0f / sqrtf(fmaf(s[1], a.inv_d, a.post_eps)) : 1.0f;
+    // D becomes q = dz * w, the gradient of the normalised row; sums of the post norm's gradient and of a token's gate
+    float u[3] = {0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int c = p.lane + i * p.stride;
+      const bool in = c < a.row_vecs;
+      float w[NE], b[NE], g[NE], dg[NE];
+      post_w.unpack(i, w);
+      post_b.unpack(i, b);
+      weight_of<NE>(a.post_w != nullptr, a.offset, w);
+      if (a.gate_kind == OCCULT_GATE_CHANNEL) cgate.unpack(i, g);
+      else if (a.gate_kind == OCCULT_GATE_ELEMENT) gr.unpack(i, g);
+      else
+#pragma unroll
+        for (int e = 0; e < NE; ++e) g[e] = token_gate;
+#pragma unroll
+      for (int e = 0; e < NE; ++e) {
+        const float hat = y[i][e] * r, sD = in ? a.y_scale * D[i][e] : 0.0f;
+        dg[e] = fmaf(hat, w[e], b[e]) * sD;
+        const float dz = g[e] * sD;
+        col[kPostW][i][e] = fmaf(dz, hat, col[kPostW][i][e]);
+        if constexpr (LAYER) col[kPostB][i][e] += dz;
+        D[i][e] = dz * w[e];
+        u[0] = fmaf(D[i][e], hat, u[0]);
+        u[1] += D[i][e];
+        u[2] += dg[e];
+        col[kGate][i][e] += dg[e];
+      }
+      if (a.gate_kind == OCCULT_GATE_ELEMENT && a.dgate && valid && in) R::store_round(a.dgate, t, a.row_vecs, c, dg);
+    }
+    if (a.post || a.gate_kind == OCCULT_GATE_TOKEN) row_sums<W>(u, a.lanes, slot);
+    if (a.gate_kind == OCCULT_GATE_TOKEN && a.dgate && valid && p.lane == 0) static_cast<float*>(a.dgate)[t] = u[2];
+    const float m2 = a.post ? u[0] * a.inv_d : 0.0f, m1 = LAYER && a.post == OCCULT_NORM_LAYER ? u[1] * a.inv_d : 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int c = p.lane + i * p.stride;
+      float v[NE];
+#pragma unroll
+      for (int e = 0; e < NE; ++e) v[e] = r * (D[i][e] - m1 - y[i][e] * r * m2);
+      if (valid && c < a.row_vecs) R::store_round(a.dy, t, a.row_vecs, c, v);
+    }
+  }
+
+  if (!a.sums) return;
+  constexpr int kThreads = Place<V, W>::kWaves * 64;
+  __shared__ float s_col[W < 4 ? kThreads * V * NE : 1];   // from four waves on a workgroup has one row at a time
+  const int d = a.row_vecs * NE;
+  float* ws = a.ws + (size_t)blockIdx.x * __popc(a.sums) * d;
+#pragma unroll
+  for (int n = 0; n < NS; ++n) {
+    // bits of `sums`: post weight, post bias, pre weight, pre bias, channel gate
+    constexpr int kBit[kColSums] = {0, 2, 4, 1, 3};
+    if (!(a.sums >> kBit[n] & 1)) continue;   // uniform
+    float* mine = s_col + (p.row * p.stride + p.lane) * V * NE;
+    __syncthreads();
+    if (p.row > 0) {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+#pragma unroll
+        for (int e = 0; e < NE; ++e) mine[i * NE + e] = col[n][i][e];
+    }
+    __syncthreads();
+    if (p.row == 0) {
+      float* dst = ws + (size_t)__popc(a.sums & ((1 << kBit[n]) - 1)) * d;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int c = p.lane + i * p.stride;
+        for (int g = 1; g < rows; ++g)
+#pragma unroll
+          for (int e = 0; e < NE; ++e) col[n][i][e] += s_col[(g * p.stride + p.lane) * V * NE + i * NE + e];
+        if (c < a.row_vecs)
+#pragma unroll
+          for (int e = 0; e < NE; ++e) dst[c * NE + e] = col[n][i][e];
+      }
+    }
+  }
+}
+
+struct ColumnArgs {
+  const float* ws;
+  float* dst[kColSums];
+  int blocks, nsums, d, accumulate;
+};
+
+// 64 columns per workgroup, 16 slices of the workgroups' sums, added in order
+__global__ __launch_bounds__(1024) void column_sums_kernel(const ColumnArgs a) {
+  __shared__ float s_part[16][64];
+  const int lane = threadIdx.x & 63, slice = threadIdx.x >> 6;
+  const long long n = (long long)a.nsums * a.d, col = (long long)blockIdx.x * 64 + lane;
+  const int lo = (int)((long long)a.blocks * slice / 16), hi = (int)((long long)a.blocks * (slice + 1) / 16);
+  float sum = 0.0f;
+  if (col < n) {
+#pragma unroll 8
+    for (int b = lo; b < hi; ++b) sum += a.ws[(size_t)b * n + col];
+  }
+  s_part[slice][lane] = sum;
+  __syncthreads();
+  if (slice == 0 && col < n) {
+#pragma unroll
+    for (int i = 1; i < 16; ++i) sum += s_part[i][lane];
+    const int which = (int)(col / a.d), c = (int)(col % a.d);
+    float* dst = a.dst[0];
+#pragma unroll
+    for (int i = 1; i < kColSums; ++i)
+      if (which == i) dst = a.dst[i];
+    dst[c] = a.accumulate ? dst[c] + sum : sum;
+  }
+}
+
+// Vectors per lane, waves per row and lanes per row of a row length: V and W of the kernels above.
+struct Shape {
+  int V, W, lanes;
+};
+static Shape shape_of(int row_vecs, int v_max) {
+  Shape s{1, 1, 64};
+  if (row_vecs <= 64) {
+    while (s.lanes > 1 && s.lanes / 2 >= row_vecs) s.lanes /= 2;
+    return s;
+  }
+  while (s.V < v_max && 64 * s.V < row_vecs) s.V *= 2;
+  while (s.W < 16 && 64 * s.V * s.W < row_vecs) s.W *= 2;
+  return s;
+}
+static int rows_per_block(const Shape& s) { return s.W == 1 ? 4 * (64 / s.lanes) : (s.W < 4 ? 4 / s.W : 1); }
+
+constexpr int kForwardV = 4, kBackwardV = 2;
+
+static int backward_blocks(const occult_cfg_t& c) {
+  const int rows = rows_per_block(shape_of(c.d * elem_size(c) / 16, kBackwardV));
+  const long long need = ((long long)c.T + rows - 1) / rows;
+  return need < kBackwardBlocks ? (int)need : kBackwardBlocks;
+}
+
+static int check(const occult_cfg_t* cfg, const occult_block_norm_t* n) {
+  int rc = check_cfg(cfg);
+  if (rc) return rc;
+  OCC_REQUIRE(n, OCCULT_ENULLPTR, "norm description is NULL");
+  const occult_cfg_t& c = *cfg;
+  const size_t row = (size_t)c.d * elem_size(c);
+  OCC_REQUIRE(row % 16 == 0, OCCULT_EALIGN, "rows of d=%d elements are not multiples of 16 bytes", c.d);
+  OCC_REQUIRE(row <= (size_t)kMaxRowBytes, OCCULT_ESHAPE, "rows of %zu bytes are longer than %d", row, kMaxRowBytes);
+  OCC_REQUIRE(n->post_kind >= OCCULT_NORM_NONE && n->post_kind <= OCCULT_NORM_LAYER && n->pre_kind >= OCCULT_NORM_NONE &&
+                  n->pre_kind <= OCCULT_NORM_LAYER,
+              OCCULT_EINVAL, "unknown norm (post %d, pre %d)", n->post_kind, n->pre_kind);
+  OCC_REQUIRE(n->gate_kind >= OCCULT_GATE_NONE && n->gate_kind <= OCCULT_GATE_ELEMENT, OCCULT_EINVAL, "unknown gate %d",
+              n->gate_kind);
+  OCC_REQUIRE(isfinite(n->x_scale) && isfinite(n->y_scale) && isfinite(n->weight_offset), OCCULT_EINVAL,
+              "x_scale, y_scale or weight_offset is not finite");
+  if (n->post_kind)
+    OCC_REQUIRE(isfinite(n->post_eps) && n->post_eps > 0.0f, OCCULT_EINVAL, "post_eps=%g must be positive", (double)n->post_eps);
+  else
+    OCC_REQUIRE(!n->post_weight && !n->post_bias, OCCULT_EINVAL, "post_weight or post_bias without a post norm");
+  if (n->pre_kind)
+    OCC_REQUIRE(isfinite(n->pre_eps) && n->pre_eps > 0.0f, OCCULT_EINVAL, "pre_eps=%g must be positive", (double)n->pre_eps);
+  else
+    OCC_REQUIRE(!n->pre_weight && !n->pre_bias, OCCULT_EINVAL, "pre_weight or pre_bias without a pre norm");
+  OCC_REQUIRE((n->gate != nullptr) == (n->gate_kind != OCCULT_GATE_NONE) || c.T == 0, OCCULT_ENULLPTR,
+              "gate and gate_kind=%d do not belong together", n->gate_kind);
+  OCC_REQUIRE(aligned16(n->post_weight) && aligned16(n->post_bias) && aligned16(n->pre_weight) && aligned16(n->pre_bias) &&
+                  (n->gate_kind == OCCULT_GATE_TOKEN || aligned16(n->gate)),
+              OCCULT_EALIGN, "a parameter is not 16-byte aligned");
+  return OCCULT_OK;
+}
+
+// column sums of a description, as bits: post weight, post bias, pre weight, pre bias, channel gate
+static int wanted_sums(const occult_block_norm_t& n) {
+  return (n.post_weight ? 1 : 0) | (n.post_bias ? 2 : 0) | (n.pre_weight ? 4 : 0) | (n.pre_bias ? 8 : 0) |
+         (n.gate_kind == OCCULT_GATE_CHANNEL ? 16 : 0);
+}
+
+static int popcount(int v) { return __builtin_popcount((unsigned)v); }
+
+template <bool BF16>
+static int launch_forward(const Args& a, const Shape& s, hipStream_t stream) {
+  const int rows = rows_per_block(s);
+  const long long need = ((long long)a.T + rows - 1) / rows;
+  const int grid = need < 4096 ? (int)need : 4096;
+#define OCC_NORM_CASE(V_, W_)                                                                             \
+  if (s.V == V_ && s.W == W_) {                                                                           \
+    block_norm_kernel<BF16, V_, W_><<<grid, Place<V_, W_>::kWaves * 64, 0, stream>>>(a);                  \
+    OCC_LAUNCH_CHECK("block_norm_kernel");                                                                \
+    return OCCULT_OK;                                                                                     \
+  }
+  OCC_NORM_CASE(1, 1)
+  OCC_NORM_CASE(2, 1)
+  OCC_NORM_CASE(4, 1)
+  OCC_NORM_CASE(4, 2)
+  OCC_NORM_CASE(4, 4)
+  OCC_NORM_CASE(4, 8)
+#undef OCC_NORM_CASE
+  OCC_FAIL(OCCULT_ESHAPE, "no kernel for rows of %d vectors", a.row_vecs);
+}
+
+template <bool BF16, bool LAYER>
+static int launch_backward(const BackwardArgs& a, const Shape& s, int grid, hipStream_t stream) {
+#define OCC_NORM_CASE(V_, W_)                                                                             \
+  if (s.V == V_ && s.W == W_) {                                                                           \
+    block_norm_backward_kernel<BF16, V_, W_, LAYER><<<grid, Place<V_, W_>::kWaves * 64, 0, stream>>>(a);  \
+    OCC_LAUNCH_CHECK("block_norm_backward_kernel");                                                       \
+    return OCCULT_OK;                                                                                     \
+  }
+  OCC_NORM_CASE(1, 1)
+  OCC_NORM_CASE(2, 1)
+  OCC_NORM_CASE(2, 2)
+  OCC_NORM_CASE(2, 4)
+  OCC_NORM_CASE(2, 8)
+  OCC_NORM_CASE(2, 16)
+#undef OCC_NORM_CASE
+  OCC_FAIL(OCCULT_ESHAPE, "no kernel for rows of %d vectors", a.row_vecs);
+}
+
+}  // namespace norm
+
+}  // namespace occult
+
+using namespace occult;
+using namespace occult::norm;
+
+extern "C" int occult_block_norm(const occult_cfg_t* cfg, const occult_block_norm_t* n, const void* x, const void* y, void* out,
+                                 void* h, occult_stream_t stream) {
+  int rc = check(cfg, n);
+  if (rc) return rc;
+  const occult_cfg_t& c = *cfg;
+  if (y == nullptr && c.T > 0)
+    OCC_REQUIRE(n->post_kind == OCCULT_NORM_NONE && n->gate_kind == OCCULT_GATE_NONE && n->pre_kind != OCCULT_NORM_NONE,
+                OCCULT_EINVAL, "without y there is nothing but a pre norm to do");
+  if (c.T == 0) return OCCULT_OK;
+  OCC_REQUIRE(x, OCCULT_ENULLPTR, "x is NULL");
+  OCC_REQUIRE(!y || out, OCCULT_ENULLPTR, "out is NULL");
+  OCC_REQUIRE(!n->pre_kind || h, OCCULT_ENULLPTR, "h is NULL with a pre norm");
+  OCC_REQUIRE(aligned16(x) && aligned16(y) && aligned16(out) && aligned16(h), OCCULT_EALIGN, "a buffer is not 16-byte aligned");
+  OCC_REQUIRE(!n->pre_kind || !y || h != out, OCCULT_EINVAL, "out and h are the same buffer");
+  Args a{};
+  a.x = x; a.y = y; a.gate = n->gate; a.out = out; a.h = h;
+  a.post_w = n->post_weight; a.post_b = n->post_bias; a.pre_w = n->pre_weight; a.pre_b = n->pre_bias;
+  a.T = c.T; a.row_vecs = c.d * elem_size(c) / 16;
+  a.post = n->post_kind; a.pre = n->pre_kind; a.gate_kind = n->gate_kind;
+  a.x_scale = n->x_scale; a.y_scale = n->y_scale; a.post_eps = n->post_eps; a.pre_eps = n->pre_eps;
+  a.offset = n->weight_offset; a.inv_d = 1.0f / (float)c.d;
+  const Shape s = shape_of(a.row_vecs, kForwardV);
+  a.lanes = s.lanes;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  return c.dtype == OCCULT_BF16 ? launch_forward<true>(a, s, st) : launch_forward<false>(a, s, st);
+}
+
+extern "C" int occult_block_norm_backward_ws_bytes(const occult_cfg_t* cfg, const occult_block_norm_t* n, size_t* ws_bytes) {
+  int rc = check(cfg, n);
+  if (rc) return rc;
+  OCC_REQUIRE(ws_bytes, OCCULT_ENULLPTR, "output pointer is NULL");
+  *ws_bytes = (size_t)backward_blocks(*cfg) * popcount(wanted_sums(*n)) * (size_t)cfg->d * 4;
+  return OCCULT_OK;
+}
+
+extern "C" int occult_block_norm_backward(const occult_cfg_t* cfg, const occult_block_norm_t* n, const void* y, const void* out,
+                                          const void* dout, const void* dh, void* dx, void* dy,
+                                          const occult_block_norm_grads_t* grads, int accumulate, void* ws, size_t ws_bytes,
+                                          occult_stream_t stream) {
+  int rc = check(cfg, n);
+  if (rc) return rc;
+  const occult_cfg_t& c = *cfg;
+  OCC_REQUIRE(accumulate == 0 || accumulate == 1, OCCULT_EINVAL, "accumulate=%d must be 0 or 1", accumulate);
+  OCC_REQUIRE(grads, OCCULT_ENULLPTR, "grads is NULL");
+  const occult_block_norm_grads_t& g = *grads;
+  OCC_REQUIRE((!g.post_weight || n->post_weight) && (!g.post_bias || n->post_bias) && (!g.pre_weight || n->pre_weight) &&
+                  (!g.pre_bias || n->pre_bias) && (!g.gate || n->gate_kind),
+              OCCULT_EINVAL, "a gradient is asked for of a parameter that is not there");
+  OCC_REQUIRE(dy || c.T == 0 || (!g.post_weight && !g.post_bias && !g.gate), OCCULT_ENULLPTR,
+              "gradients of the post norm or the gate without dy");
+  OCC_REQUIRE(aligned16(y) && aligned16(out) && aligned16(dout) && aligned16(dh) && aligned16(dx) && aligned16(dy) && aligned16(ws) &&
+                  aligned16(g.gate) && aligned16(g.post_weight) && aligned16(g.post_bias) && aligned16(g.pre_weight) &&
+                  aligned16(g.pre_bias),
+              OCCULT_EALIGN, "a buffer is not 16-byte aligned");
+  float* const all[kColSums] = {g.post_weight, g.post_bias, g.pre_weight, g.pre_bias,
+                                n->gate_kind == OCCULT_GATE_CHANNEL ? static_cast<float*>(g.gate) : nullptr};
+  int sums = 0;
+  for (int i = 0; i < kColSums; ++i) sums |= all[i] ? 1 << i : 0;
+  const int blocks = backward_blocks(c);
+  if (c.T > 0) {
+    OCC_REQUIRE(!n->pre_kind || (out && dh), OCCULT_ENULLPTR, "out or dh is NULL with a pre norm");
+    OCC_REQUIRE(n->pre_kind || dout, OCCULT_ENULLPTR, "dout is NULL without a pre norm");
+    OCC_REQUIRE(dx || dy, OCCULT_ENULLPTR, "dx and dy are NULL");
+    OCC_REQUIRE(!dy || y || (!n->post_kind && !n->gate_kind), OCCULT_ENULLPTR, "y is NULL with a post norm or a gate");
+    OCC_REQUIRE(dx != dy, OCCULT_EINVAL, "dx and dy are the same buffer");
+    if (sums)
+      OCC_REQUIRE(ws && ws_bytes >= (size_t)blocks * popcount(sums) * (size_t)c.d * 4, OCCULT_EWORKSPACE,
+                  "workspace of %zu bytes < required %zu", ws ? ws_bytes : (size_t)0, (size_t)blocks * popcount(sums) * (size_t)c.d * 4);
+  }
+  BackwardArgs a{};
+  a.y = y; a.out = out; a.dout = dout; a.dh = dh; a.gate = n->gate; a.dx = dx; a.dy = dy; a.dgate = g.gate;
+  a.post_w = n->post_weight; a.post_b = n->post_bias; a.pre_w = n->pre_weight;
+  a.ws = static_cast<float*>(ws);
+  a.T = c.T; a.row_vecs = c.d * elem_size(c) / 16;
+  a.post = n->post_kind; a.pre = n->pre_kind; a.gate_kind = n->gate_kind; a.sums = sums;
+  a.x_scale = n->x_scale; a.y_scale = n->y_scale; a.post_eps = n->post_eps; a.pre_eps = n->pre_eps;
+  a.offset = n->weight_offset; a.inv_d = 1.0f / (float)c.d;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (c.T > 0) {
+    const Shape s = shape_of(a.row_vecs, kBackwardV);
+    a.lanes = s.lanes;
+    const bool layer = n->post_kind == OCCULT_NORM_LAYER || n->pre_kind == OCCULT_NORM_LAYER || (sums & 10);
+    if (c.dtype == OCCULT_BF16)
+      rc = layer ? launch_backward<true, true>(a, s, blocks, st) : launch_backward<true, false>(a, s, blocks, st);
+    else
+      rc = layer ? launch_backward<false, true>(a, s, blocks, st) : launch_backward<false, false>(a, s, blocks, st);
+    if (rc) return rc;
+  }
+  if (sums && (c.T > 0 || !accumulate)) {
+    ColumnArgs ca{};
+    ca.ws = a.ws;
+    ca.blocks = c.T > 0 ? blocks : 0;
+    ca.d = c.d;
+    ca.accumulate = accumulate;
+    for (int i = 0; i < kColSums; ++i)
+      if (all[i]) ca.dst[ca.nsums++] = all[i];
+    const long long cols = (long long)ca.nsums * c.d;
+    column_sums_kernel<<<(int)((cols + 63) / 64), 1024, 0, st>>>(ca);
+    OCC_LAUNCH_CHECK("column_sums_kernel");
+  }
+  return OCCULT_OK;
+}
