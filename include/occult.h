@@ -258,6 +258,45 @@ int occult_expert_ffn_packed(const occult_cfg_t* cfg, const occult_plan_t* plan,
                              void* epd_h, void* epd_y, void* h_shared, void* y_shared, void* ws,
                              size_t ws_bytes, occult_stream_t stream);
 
+/* 4-bit expert weights with group scales, for serving from a quarter of the memory (decoding streams the active experts' weights
+ * once per step): weight k of a row of K is
+ *   scale[k / group] * (code[k] - zero[k / group]),   code 0..15, group 32, 64 or 128 (a row's last group may be shorter),
+ * scales bf16 in layers of either dtype, zero points 0..15 or, with zeros[] NULL, 8 everywhere.  Device ptrs, in the order gate, up, down;
+ * the rows are those of occult_weights_t:
+ *   codes  [E+S][rows][K / 2]             two codes per byte, the lower k in the low bits; 16-byte aligned
+ *   scales [E+S][rows][ceil(K / group)]   zeros [E+S][rows][ceil(K / group)]
+ * (gate, up: rows f, K d; down: rows d, K f).  Rows of x, h and y are 16-byte multiples as everywhere; no other condition on d, f.
+ *
+ * occult_quantize_weights writes them from weights in cfg.dtype (finite), rounding to nearest: scale = bf16 of max|w| / 7, or with
+ *   zeros[] given of (max(w, 0) - min(w, 0)) / 15; zero = round(-min / scale); code = round(w / scale) + zero, clamped.
+ *   A group of zeros gets scale 0 and codes 8.
+ * occult_dequantize_weights writes the values they stand for in cfg.dtype, in the layout of occult_weights_t (rounded to nearest): for
+ *   batches of hundreds of rows per expert, where occult_expert_ffn on them is the faster way.
+ * occult_pack_w4 writes codes and scales in the order the products read them (occult_pack_w4_bytes() bytes, 16-byte aligned; nothing
+ *   else is read afterwards): per matrix (gate and up in pairs) units of 16 rows, per unit K blocks of 128, per block and
+ *   matrix 64 pieces of 16 bytes, piece l = row l % 16, whose dword j holds K elements j * 32 + (l / 16) * 8 .. + 8: element 2i in bits
+ *   4i .. 4i + 3, 2i + 1 in bits 16 + 4i .., rotated left by 3.  Scales follow the codes of all matrices in the same order.
+ * occult_expert_ffn_w4 is occult_expert_ffn computed from them: same plan, same rows, same outputs; products of x and codes are
+ *   summed in f32 per group and scaled in f32 (f32 layers: x is not rounded either); h is rounded to cfg.dtype between the
+ *   two products.  cfg.ffn_phase as there.  Row sums do not depend on T within a rule on T * k / E that picks the tile.
+ * occult_forward_w4 is occult_forward with occult_expert_ffn_w4 in the place of the expert computation (no pre-activations
+ *   are kept: buffers->epd_gu, gu_shared and ffn_ws are not used). */
+typedef struct occult_w4_weights {
+  int32_t   group;
+  uint8_t*  codes[3];
+  uint16_t* scales[3];
+  uint8_t*  zeros[3];
+} occult_w4_weights_t;
+int occult_quantize_weights(const occult_cfg_t* cfg, const occult_weights_t* weights, const occult_w4_weights_t* out,
+                            occult_stream_t stream);
+int occult_dequantize_weights(const occult_cfg_t* cfg, const occult_w4_weights_t* q, void* w_gate, void* w_up, void* w_down,
+                              occult_stream_t stream);
+int occult_pack_w4_bytes(const occult_cfg_t* cfg, int group, int zeros, size_t* bytes);
+int occult_pack_w4(const occult_cfg_t* cfg, const occult_w4_weights_t* q, void* packed, size_t packed_size, occult_stream_t stream);
+int occult_expert_ffn_w4(const occult_cfg_t* cfg, const occult_plan_t* plan, const void* sfd_x, const void* x, const void* packed,
+                         size_t packed_size, int group, int zeros, void* epd_h, void* epd_y, void* h_shared, void* y_shared,
+                         occult_stream_t stream);
+
 /* Two-stage combine (paper Sec. 3.1 two-stage aggregation of Eq. 0; App. A.2 "Weight
  * Modulation", the accumulation of "SMM with Merging", and "Combine").
  * Stage 1 (on the device, before the return trip): sfd_y[r] = sum over the EPD rows q of SFD
@@ -293,6 +332,9 @@ typedef struct occult_forward_buffers {
 int occult_forward(const occult_cfg_t* cfg, const occult_plan_t* plan, const float* logits, const void* x,
                    const occult_weights_t* weights, const void* packed,
                    const occult_forward_buffers_t* buffers, occult_stream_t stream);
+
+int occult_forward_w4(const occult_cfg_t* cfg, const occult_plan_t* plan, const float* logits, const void* x, const void* packed,
+                      size_t packed_size, int group, int zeros, const occult_forward_buffers_t* buffers, occult_stream_t stream);
 
 /* occult_combine with the paper's own first stage, an atomic merge (paper Sec. 3.1, first-stage merging: thread
  * blocks that write the same SFD rows add with atomic_add into a float32 output tensor that is converted to the

@@ -31,6 +31,8 @@ EXPORTS = [
     "occult_collaboration_stats", "occult_plan_static", "occult_combine_atomic",
     "occult_expert_ffn_backward_weights_ws_bytes", "occult_expert_ffn_backward_weights_ws", "occult_forward",
     "occult_block_norm", "occult_block_norm_backward", "occult_block_norm_backward_ws_bytes",
+    "occult_quantize_weights", "occult_dequantize_weights", "occult_pack_w4_bytes", "occult_pack_w4", "occult_expert_ffn_w4",
+    "occult_forward_w4",
 ]
 
 
@@ -62,6 +64,10 @@ class occult_forward_buffers_t(Structure):
     _fields_ = [(n, c_void_p) for n in ("ids", "w", "plan_ws", "sfd_x", "epd_h", "epd_y", "h_shared", "y_shared", "ffn_ws",
                                         "epd_gu", "gu_shared", "sfd_y", "y")] + [
                 ("plan_ws_bytes", c_size_t), ("ffn_ws_bytes", c_size_t)]
+
+
+class occult_w4_weights_t(Structure):
+    _fields_ = [("group", c_int32), ("codes", c_void_p * 3), ("scales", c_void_p * 3), ("zeros", c_void_p * 3)]
 
 
 class occult_block_norm_t(Structure):
@@ -138,6 +144,14 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.occult_placement_greedy.argtypes = [c_void_p, c_int32, c_int32, c_void_p, c_void_p]
     lib.occult_collaboration_stats.argtypes = [c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p]
     lib.occult_plan_stats.argtypes = [cfgp, planp, POINTER(occult_stats_t), c_void_p]
+    w4p = POINTER(occult_w4_weights_t)
+    lib.occult_quantize_weights.argtypes = [cfgp, POINTER(occult_weights_t), w4p, c_void_p]
+    lib.occult_dequantize_weights.argtypes = [cfgp, w4p] + [c_void_p] * 4
+    lib.occult_pack_w4_bytes.argtypes = [cfgp, c_int, c_int, POINTER(c_size_t)]
+    lib.occult_pack_w4.argtypes = [cfgp, w4p, c_void_p, c_size_t, c_void_p]
+    lib.occult_expert_ffn_w4.argtypes = [cfgp, planp] + [c_void_p] * 3 + [c_size_t, c_int, c_int] + [c_void_p] * 5
+    lib.occult_forward_w4.argtypes = [cfgp, planp] + [c_void_p] * 3 + [c_size_t, c_int, c_int, POINTER(occult_forward_buffers_t),
+                                                                       c_void_p]
     normp = POINTER(occult_block_norm_t)
     lib.occult_block_norm.argtypes = [cfgp, normp] + [c_void_p] * 5
     lib.occult_block_norm_backward_ws_bytes.argtypes = [cfgp, normp, POINTER(c_size_t)]
@@ -430,6 +444,53 @@ def occult_plan_stats(cfg, plan, stream=None) -> occult_stats_t:
     _check(load_library().occult_plan_stats(ctypes.byref(cfg), ctypes.byref(plan), ctypes.byref(st),
                                             _stream(stream)))
     return st
+
+
+def _w4(group, codes, scales, zeros) -> occult_w4_weights_t:
+    """codes, scales, zeros: three tensors each, in the order gate, up, down (zeros: None or three Nones without zero points)."""
+    q = occult_w4_weights_t(int(group))
+    for i in range(3):
+        q.codes[i], q.scales[i] = _ptr(codes[i]), _ptr(scales[i])
+        q.zeros[i] = None if zeros is None else _ptr(zeros[i])
+    return q
+
+
+def occult_quantize_weights(cfg, w_gate, w_up, w_down, group, codes, scales, zeros=None, stream=None) -> None:
+    wts = occult_weights_t(_ptr(w_gate), _ptr(w_up), _ptr(w_down))
+    _check(load_library().occult_quantize_weights(ctypes.byref(cfg), ctypes.byref(wts), ctypes.byref(_w4(group, codes, scales, zeros)),
+                                                  _stream(stream)))
+
+
+def occult_dequantize_weights(cfg, group, codes, scales, zeros, w_gate, w_up, w_down, stream=None) -> None:
+    _check(load_library().occult_dequantize_weights(ctypes.byref(cfg), ctypes.byref(_w4(group, codes, scales, zeros)), _ptr(w_gate),
+                                                    _ptr(w_up), _ptr(w_down), _stream(stream)))
+
+
+def occult_pack_w4_bytes(cfg, group, zeros=False) -> int:
+    n = c_size_t(0)
+    _check(load_library().occult_pack_w4_bytes(ctypes.byref(cfg), int(group), int(bool(zeros)), ctypes.byref(n)))
+    return int(n.value)
+
+
+def occult_pack_w4(cfg, group, codes, scales, zeros, packed, stream=None) -> None:
+    _check(load_library().occult_pack_w4(ctypes.byref(cfg), ctypes.byref(_w4(group, codes, scales, zeros)), _ptr(packed),
+                                         packed.numel() * packed.element_size(), _stream(stream)))
+
+
+def occult_expert_ffn_w4(cfg, plan, sfd_x, x, packed, group, zeros, epd_h, epd_y, h_shared=None, y_shared=None, stream=None) -> None:
+    _check(load_library().occult_expert_ffn_w4(ctypes.byref(cfg), ctypes.byref(plan), _ptr(sfd_x), _ptr(x), _ptr(packed),
+                                               packed.numel() * packed.element_size(), int(group), int(bool(zeros)), _ptr(epd_h),
+                                               _ptr(epd_y), _ptr(h_shared), _ptr(y_shared), _stream(stream)))
+
+
+def occult_forward_w4(cfg, plan, logits, x, packed, group, zeros, ids, w, plan_ws, sfd_x, epd_h, epd_y, h_shared, y_shared, sfd_y, y,
+                      stream=None) -> None:
+    buf = occult_forward_buffers_t(_ptr(ids), _ptr(w), _ptr(plan_ws), _ptr(sfd_x), _ptr(epd_h), _ptr(epd_y), _ptr(h_shared),
+                                   _ptr(y_shared), None, None, None, _ptr(sfd_y), _ptr(y),
+                                   plan_ws.numel() * plan_ws.element_size(), 0)
+    _check(load_library().occult_forward_w4(ctypes.byref(cfg), ctypes.byref(plan), _ptr(logits), _ptr(x), _ptr(packed),
+                                            packed.numel() * packed.element_size(), int(group), int(bool(zeros)), ctypes.byref(buf),
+                                            _stream(stream)))
 
 
 def make_block_norm(post_kind, pre_kind, gate_kind, x_scale=1.0, y_scale=1.0, post_eps=1e-6, pre_eps=1e-6, weight_offset=0.0,

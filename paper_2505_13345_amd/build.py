@@ -20,7 +20,7 @@ OBJ_DIR = os.path.join(ROOT, "_build", "occult")
 LIB_PATH = os.path.join(HERE, "liboccult.so")
 
 SOURCES = ["api.hip", "route.hip", "plan.hip", "dispatch.hip", "ffn.hip", "ffn_tile128.hip", "combine.hip", "combine_atomic.hip", "coact.hip", "backward.hip",
-           "ffn_backward.hip", "wgrad.hip", "norm.hip"]
+           "ffn_backward.hip", "wgrad.hip", "norm.hip", "w4.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",

@@ -8,10 +8,25 @@ synchronises or computes.  Table views onto the plan block are for tests and rep
 from __future__ import annotations
 
 import operator
+from typing import NamedTuple, Optional
 
 import torch
 
 from . import binding as B
+
+
+class W4Weights(NamedTuple):
+    """Expert weights in 4 bits, weight = scale * (code - zero), each field three tensors in the order gate, up, down:
+    codes uint8 [E+S, rows, K / 2] (two along K per byte, the lower one in the low bits), scales bfloat16 and zeros uint8
+    [E+S, rows, ceil(K / group)]; zeros is None, or three Nones, where every zero point is 8."""
+    group: int
+    codes: tuple
+    scales: tuple
+    zeros: Optional[tuple] = None
+
+    @property
+    def has_zeros(self):
+        return self.zeros is not None and self.zeros[0] is not None
 
 
 class OccultLayer:
@@ -138,6 +153,95 @@ class OccultLayer:
         T, k, f, S = s["T"], s["k"], s["f"], s["S"]
         return (self._buf("epd_gu", (T * k, 2 * f), self.tdtype),
                 self._buf("gu_shared", (T, S * 2 * f), self.tdtype) if S > 0 else None)
+
+    # ---- 4-bit weights -------------------------------------------------------------------------
+    def _w4_shapes(self, group):
+        s = self.shape
+        n = s["E"] + s["S"]
+        return [(n, rows, K, (K + group - 1) // group) for rows, K in ((s["f"], s["d"]), (s["f"], s["d"]), (s["d"], s["f"]))]
+
+    def _expect_w4(self, w4):
+        B.occult_pack_w4_bytes(self.cfg, w4.group, w4.has_zeros)   # refuses the group and the layer's rows
+        for i, ((n, rows, K, groups), name) in enumerate(zip(self._w4_shapes(w4.group), ("gate", "up", "down"))):
+            B.expect(w4.codes[i], f"codes of {name}", torch.uint8, n * rows * K // 2)
+            B.expect(w4.scales[i], f"scales of {name}", torch.bfloat16, n * rows * groups)
+            if w4.has_zeros:
+                B.expect(w4.zeros[i], f"zeros of {name}", torch.uint8, n * rows * groups)
+
+    def quantize_weights(self, w_gate, w_up, w_down, group=128, zeros=False):
+        """The layer's weights rounded to 4 bits with a scale (and, if asked for, a zero point) per `group` weights along K."""
+        self._weights(w_gate, w_up, w_down)
+        B.occult_pack_w4_bytes(self.cfg, group, zeros)
+        shapes = self._w4_shapes(group)
+        empty = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=self.device)
+        w4 = W4Weights(group, tuple(empty((n, rows, K // 2), torch.uint8) for n, rows, K, _ in shapes),
+                       tuple(empty((n, rows, g), torch.bfloat16) for n, rows, _, g in shapes),
+                       tuple(empty((n, rows, g), torch.uint8) for n, rows, _, g in shapes) if zeros else None)
+        B.occult_quantize_weights(self.cfg, w_gate, w_up, w_down, *w4)
+        return w4
+
+    def dequantize_weights(self, w4):
+        """The values that 4-bit weights stand for, in the layer's type: w_gate, w_up, w_down for forward() on large batches."""
+        self._expect_w4(w4)
+        w = tuple(torch.empty((n, rows, K), dtype=self.tdtype, device=self.device) for n, rows, K, _ in self._w4_shapes(w4.group))
+        B.occult_dequantize_weights(self.cfg, *w4, *w)
+        return w
+
+    def pack_weights_w4(self, w4):
+        """4-bit weights in the order that expert_ffn_w4() and forward_w4() read (again after every change of the weights, which
+        are not read after this)."""
+        self._expect_w4(w4)
+        n = B.occult_pack_w4_bytes(self.cfg, w4.group, w4.has_zeros)
+        if getattr(self, "packed_w4", None) is None or self.packed_w4.numel() < n:
+            self.packed_w4 = torch.empty(n, dtype=torch.uint8, device=self.device)
+        self.w4_format = (w4.group, w4.has_zeros)
+        B.occult_pack_w4(self.cfg, *w4, self.packed_w4)
+        return self.packed_w4
+
+    def _packed_w4(self):
+        if getattr(self, "packed_w4", None) is None:
+            raise ValueError("occult: no 4-bit weights: call pack_weights_w4() first")
+        return (self.packed_w4, *self.w4_format)
+
+    def expert_ffn_w4(self, x):
+        """expert_ffn() from 4-bit weights -> epd_y, y_shared (None without shared experts)."""
+        self._hidden(x, "x")
+        self.gu_saved = False
+        B.occult_expert_ffn_w4(self.cfg, self.plan, self.sfd_x, x, *self._packed_w4(), self.epd_h, self.epd_y, self.h_shared,
+                               self.y_shared)
+        return self.epd_y, self.y_shared
+
+    def forward_w4(self, logits, x):
+        """forward() from 4-bit weights."""
+        if _w4_steps_of(type(self)) != _W4_STEPS or not self.__dict__.keys().isdisjoint(_W4_STEP_NAMES):
+            self.route(logits)
+            self.make_plan()
+            self.dispatch(x)
+            self.expert_ffn_w4(x)
+            self.combine()
+            return self.y
+        s = self.shape
+        B.expect(logits, "logits", torch.float32, s["T"] * s["E"])
+        self._hidden(x, "x")
+        self.gu_saved = False
+        B.occult_forward_w4(self.cfg, self.plan, logits, x, *self._packed_w4(), self.ids, self.w, self.ws, self.sfd_x, self.epd_h,
+                            self.epd_y, self.h_shared, self.y_shared, self.sfd_y, self.y)
+        return self.y
+
+    def forward_block(self, x, h, w_router, norm, weights=None, **params):
+        """The layer inside its block: router scores of h [T, d] (the normed residual stream), the experts (weights = w_gate, w_up,
+        w_down, or None for the 4-bit ones), and norm.forward(x, y, **params), a norm.BlockNorm that adds y to the residual stream x
+        and norms it for the next block -> out, the next block's h.  Router scores stay in self.logits."""
+        s = self.shape
+        self.route_from_hidden(h, w_router, self._buf("logits", (s["T"], s["E"]), torch.float32))
+        self.make_plan()
+        self.dispatch(h)
+        if weights is None:
+            self.expert_ffn_w4(h)
+        else:
+            self.expert_ffn(h, *weights)
+        self.combine()
+        return norm.forward(x, self.y, **params)
 
     def combine(self, epd_y=None):
         self._hidden(epd_y, "epd_y", self.shape["T"] * self.shape["k"])
@@ -315,3 +419,6 @@ class OccultLayer:
 _STEP_NAMES = ("route", "make_plan", "dispatch", "expert_ffn", "expert_ffn_train", "combine")
 _steps_of = operator.attrgetter(*_STEP_NAMES)
 _STEPS = _steps_of(OccultLayer)
+_W4_STEP_NAMES = ("route", "make_plan", "dispatch", "expert_ffn_w4", "combine")
+_w4_steps_of = operator.attrgetter(*_W4_STEP_NAMES)
+_W4_STEPS = _w4_steps_of(OccultLayer)
