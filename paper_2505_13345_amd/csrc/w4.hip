@@ -68,10 +68,17 @@ struct Args {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-__device__ __forceinline__ bf16x8 operand_of(unsigned v) {
-  constexpr unsigned kMask = 0x00780078u, kSixteen = 0x41804180u;
-  const u32x4 r = {(v & kMask) | kSixteen, (__builtin_amdgcn_alignbit(v, v, 4) & kMask) | kSixteen,
-                   (__builtin_amdgcn_alignbit(v, v, 8) & kMask) | kSixteen, (__builtin_amdgcn_alignbit(v, v, 12) & kMask) | kSixteen};
+// `sixteen`: 0x41804180, two bf16 16, in a vector register that the compiler does not know the value of: it then makes one and-or of the
+// two operations, which takes one constant from a scalar register and none from the instruction
+__device__ __forceinline__ unsigned two_sixteens() {
+  unsigned v = 0x41804180u;
+  asm volatile("" : "+v"(v));
+  return v;
+}
+__device__ __forceinline__ bf16x8 operand_of(unsigned v, unsigned sixteen) {
+  constexpr unsigned kMask = 0x00780078u;
+  const u32x4 r = {(v & kMask) | sixteen, (v >> 4 & kMask) | sixteen, (v >> 8 & kMask) | sixteen,
+                   (__builtin_amdgcn_alignbit(v, v, 12) & kMask) | sixteen};
   return __builtin_bit_cast(bf16x8, r);
 }
 // the inverse: 8 codes of consecutive K elements -> the dword that operand_of reads
@@ -86,6 +93,42 @@ __device__ __forceinline__ bf16x8 splat_bf16(unsigned bits) {
   const u32x4 r = {two, two, two, two};
   return __builtin_bit_cast(bf16x8, r);
 }
+
+// code - zero itself as an operand, for f32 layers: three times the instructions, and no sum of 16 * x to be taken off again (an f32
+// result would show the last bits that cancelling it costs)
+__device__ __forceinline__ bf16x8 exact_operand_of(unsigned v, unsigned sixteen, float minus_zero) {
+  const u32x4 biased = __builtin_bit_cast(u32x4, operand_of(v, sixteen));
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    r[i] = __float_as_uint(bf16_lo(biased[i]) + minus_zero) >> 16 | (__float_as_uint(bf16_hi(biased[i]) + minus_zero) & 0xFFFF0000u);
+  return __builtin_bit_cast(bf16x8, r);
+}
+
+// A lane's codes and scales of a K block of one weight matrix, as loaded (nothing is computed from them before they are used, or the
+// computation would wait for the load): G scales, in pairs of bf16, or with zero points in words of scale and -(16 + zero).
+template <int G, bool ZERO>
+struct Block {
+  static constexpr int kScaleBytes = G * (ZERO ? 4 : 2), kWords = ZERO ? G : (G + 1) / 2;
+  u32x4 q;
+  unsigned s[kWords];
+  __device__ __forceinline__ void load(const char* codes, const char* scales, unsigned lane16, unsigned scale_off) {
+    q = *reinterpret_cast<const u32x4*>(codes + (size_t)lane16);
+    const char* sp = scales + (size_t)scale_off;
+    if constexpr (kScaleBytes == 2) s[0] = *reinterpret_cast<const uint16_t*>(sp);
+    else {
+      typedef unsigned Words __attribute__((ext_vector_type(kWords)));
+      const Words w = *reinterpret_cast<const Words*>(sp);
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) s[i] = w[i];
+    }
+  }
+  __device__ __forceinline__ float scale(int g) const {
+    if constexpr (ZERO) return __uint_as_float(s[g] & 0xFFFF0000u);
+    else return __uint_as_float(g & 1 ? s[g / 2] & 0xFFFF0000u : s[g / 2] << 16);
+  }
+  __device__ __forceinline__ float minus_zero(int g) const { return ZERO ? __uint_as_float(s[ZERO ? g : 0] << 16) : -24.0f; }
+};
 
 // 8 elements of x along K as matrix operands: one, or three whose sum they are (truncations: the rest is exact every time)
 template <bool F32>
@@ -129,180 +172,416 @@ struct XFrag<true> {
   }
 };
 
+// Row tile and column block of a workgroup.  Workgroups [0, b_blocks) work on the second problem (the shared experts, whose down
+// projection has the longest K: they start first), the rest on the first.  The row tiles that read the same weights get ids 8
+// apart: they run on the same XCD, at about the same time, and all but the first find the codes in its L2 (500 tokens, 6 of 64 experts:
+// with the tiles spread over the XCDs the codes came 2.4 times from memory).  A pair (group, column block) belongs to XCD
+// (group * n_cb + block) % 8, so that column blocks that are no multiple of 8 leave no XCD with more of them.
+// b_rows, b_units: rows and units of a workgroup of the second problem.
+// group = -1: nothing to do.  Called by the whole workgroup, whose first wave does the work.
+struct Place {
+  TileInfo ti;
+  int cb;
+};
+template <int BM>
+__device__ __forceinline__ Place find_place(const Args& first, const Args& second, int b_blocks, int units_per_block, int b_rows,
+                                            int b_units, Place* s_place) {
+  if (threadIdx.x < 64) {
+    const int bid = (int)blockIdx.x, lane = threadIdx.x;
+    const GemmArgs& g = (bid < b_blocks ? second : first).g;
+    const int per_block = bid < b_blocks ? b_units : units_per_block;
+    const int n_cb = ((g.N + kUnit - 1) / kUnit + per_block - 1) / per_block;
+    Place p;
+    p.ti.group = -1;
+    p.ti.m0 = p.ti.rows = p.ti.row_base = p.cb = 0;
+    if (bid < b_blocks) {
+      const int tiles = (g.M + b_rows - 1) / b_rows;
+      const int unit = bid / (8 * tiles) * 8 + (bid & 7);
+      if (unit < g.ngroups * n_cb) {
+        p.ti.group = unit / n_cb;
+        p.ti.m0 = (bid >> 3) % tiles * b_rows;
+        p.ti.rows = g.M;
+        p.cb = unit % n_cb;
+      }
+      if (lane == 0) *s_place = p;
+    } else {
+      const int xcd = (bid - b_blocks) & 7, at = (bid - b_blocks) >> 3;
+      if (lane == 0) *s_place = p;
+      int before = 0;   // workgroups of this XCD before the groups at hand
+      for (int c0 = 0; c0 < g.ngroups; c0 += 64) {
+        const int group = c0 + lane;
+        const int lo = group < g.ngroups ? g.grp_offset[group] : 0, hi = group < g.ngroups ? g.grp_offset[group + 1] : 0;
+        const int tiles = (hi - lo + BM - 1) / BM;
+        const int cb0 = (xcd - group * n_cb) & 7;   // this group's first column block on this XCD
+        const int mine = cb0 < n_cb ? (n_cb - cb0 + 7) / 8 : 0;
+        int incl = tiles * mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+          const int v = __shfl_up(incl, o, 64);
+          if (lane >= o) incl += v;
+        }
+        const int excl = before + incl - tiles * mine;
+        if (at >= excl && at < excl + tiles * mine) {   // at most one lane over all chunks
+          p.ti.group = group;
+          p.ti.m0 = (at - excl) % tiles * BM;
+          p.ti.rows = hi - lo;
+          p.ti.row_base = lo;
+          p.cb = cb0 + (at - excl) / tiles * 8;
+          *s_place = p;
+        }
+        before += __shfl(incl, 63, 64);
+        if (before > at) break;   // uniform
+      }
+    }
+  }
+  __syncthreads();
+  Place p = *s_place;
+  p.ti.group = __builtin_amdgcn_readfirstlane(p.ti.group);
+  p.ti.m0 = __builtin_amdgcn_readfirstlane(p.ti.m0);
+  p.ti.rows = __builtin_amdgcn_readfirstlane(p.ti.rows);
+  p.ti.row_base = __builtin_amdgcn_readfirstlane(p.ti.row_base);
+  p.cb = __builtin_amdgcn_readfirstlane(p.cb);
+  return p;
+}
+
 // The four waves of a workgroup take the quarters of K of NB units of 16 output columns (NW matrices each: gate and up, or down) for up
-// to 16 * MT rows of one group, and add their sums through LDS in the order of K.  G: scales per row and K block; ZERO: with zero points.
-template <int MT, int NB, int NW, int G, bool ZERO, bool F32>
-__global__ __launch_bounds__(256) void w4_gemm(const Args first, const Args second, const int a_blocks) {
-  constexpr int BM = 16 * MT;
+// to 16 rows of one group, and add their sums through LDS in the order of K.  For few rows, where the length of a wave's stream is
+// what counts: every wave has kRing - 1 K blocks in flight.
+template <int NB, int NW, int G, bool ZERO, bool F32>
+__device__ __forceinline__ void split_product(const Args& a, const TileInfo& ti, int unit0, float (*s_red)[NB * NW * 4][64]) {
   constexpr int kSteps = kBlockK / 32, kGroupSteps = kSteps / G;
   constexpr int P = XFrag<F32>::kParts;
-  constexpr int kScaleBytes = (ZERO ? 4 : 2);
-  __shared__ TileInfo s_info;
-  int bid = (int)blockIdx.x;
-  const bool is_second = bid >= a_blocks;   // uniform
-  const Args& a = is_second ? second : first;
-  const int units = (a.g.N + kUnit - 1) / kUnit, n_cb = (units + NB - 1) / NB;
-  int mt, cb;
-  if (!is_second) {
-    mt = bid / n_cb;
-    cb = bid % n_cb;
-  } else {   // the row tiles that read the same weights 8 ids apart: on the same XCD, whose L2 then has them
-    const int b = bid - a_blocks;
-    const int tiles = (a.g.M + BM - 1) / BM;
-    const int unit = b / (8 * tiles) * 8 + (b & 7), m = (b >> 3) % tiles;
-    if (unit >= a.g.ngroups * n_cb) return;
-    mt = unit / n_cb * tiles + m;
-    cb = unit % n_cb;
-  }
-  TileInfo ti = find_tile<BM>(a.g, mt, &s_info);
-  if (ti.group < 0) return;
-  ti.group = __builtin_amdgcn_readfirstlane(ti.group);
-  ti.m0 = __builtin_amdgcn_readfirstlane(ti.m0);
-  ti.rows = __builtin_amdgcn_readfirstlane(ti.rows);
-  ti.row_base = __builtin_amdgcn_readfirstlane(ti.row_base);
+  constexpr int kRing = F32 ? 2 : 4;
+  typedef Block<G, ZERO> B;
+  const int units = (a.g.N + kUnit - 1) / kUnit;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, c = lane >> 4;
-  const int unit0 = cb * NB;
   const long long matrix = __builtin_amdgcn_readfirstlane(a.g.grp_widx ? a.g.grp_widx[ti.group] : a.g.w_base + ti.group);
-  const int nblk = min(MT, (ti.rows - ti.m0 + 15) / 16);   // token blocks with any valid row
+  // this wave's K blocks, counted through the matrices that K walks
+  const int blocks = a.kblocks * a.mats;
+  const int kb_begin = blocks * wave / 4, kb_end = blocks * (wave + 1) / 4;
 
-  const char* xrow[MT];
-#pragma unroll
-  for (int tb = 0; tb < MT; ++tb) {
-    int lr = ti.m0 + tb * 16 + r;
+  const char* xrow;
+  {
+    int lr = ti.m0 + r;
     if (lr >= ti.rows) lr = ti.rows - 1;   // rows past the group's end repeat its last one; dropped at the end
     const long long logical = ti.row_base + lr;
     const long long src = a.g.a_rows ? a.g.a_rows[logical] : logical;
-    xrow[tb] = static_cast<const char*>(a.g.A) + src * a.g.lda * (F32 ? 4 : 2);
+    xrow = static_cast<const char*>(a.g.A) + src * a.g.lda * (F32 ? 4 : 2);
   }
-
+  const unsigned lane16 = lane * 16, scale_off = r * B::kScaleBytes;
   struct Stage {
-    u32x4 q[NB][NW];
-    unsigned s[NB][NW][G];   // bf16 scale in the high half; with zero points the bf16 of -(16 + zero) in the low one
-    XFrag<F32> x[MT][kSteps];
+    B w[NB][NW];
+    XFrag<F32> x[kSteps];
   };
-  // one K block: kb counts through the matrices that K walks
   auto load = [&](Stage& st, int kb) {
-    const int mat = kb / a.kblocks, kin = kb - mat * a.kblocks;
-    const long long w = matrix + mat;
+    const int mat = a.mats == 1 ? 0 : kb / a.kblocks, kin = kb - mat * a.kblocks;   // uniform
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       const int unit = min(unit0 + nb, units - 1);   // past the last unit: read it again, dropped at the end
       const long long block = ((long long)unit * a.kblocks + kin) * NW;
 #pragma unroll
-      for (int m = 0; m < NW; ++m) {
-        st.q[nb][m] = *reinterpret_cast<const u32x4*>(a.codes + w * a.code_stride + (block + m) * kBlockBytes + lane * 16);
-        const char* sp = a.scales + w * a.scale_stride + ((block + m) * kUnit + r) * (G * kScaleBytes);
-#pragma unroll
-        for (int i = 0; i < G; ++i) {
-          if constexpr (ZERO) st.s[nb][m][i] = reinterpret_cast<const unsigned*>(sp)[i];
-          else st.s[nb][m][i] = (unsigned)reinterpret_cast<const uint16_t*>(sp)[i] << 16;
-        }
-      }
+      for (int m = 0; m < NW; ++m)
+        st.w[nb][m].load(a.codes + (matrix + mat) * a.code_stride + (block + m) * kBlockBytes,
+                         a.scales + (matrix + mat) * a.scale_stride + (block + m) * (kUnit * B::kScaleBytes), lane16, scale_off);
     }
 #pragma unroll
-    for (int tb = 0; tb < MT; ++tb)
-      if (tb < nblk) {
-#pragma unroll
-        for (int j = 0; j < kSteps; ++j)
-          st.x[tb][j].load(xrow[tb] + (size_t)mat * a.g.kseg * (F32 ? 4 : 2), kin * kBlockK + j * 32 + c * 8, a.g.kseg);
-      }
+    for (int j = 0; j < kSteps; ++j)
+      st.x[j].load(xrow + (size_t)mat * a.g.kseg * (F32 ? 4 : 2), kin * kBlockK + j * 32 + c * 8, a.g.kseg);
   };
 
-  f32x4 acc[NB][NW][MT];
+  f32x4 acc[NB][NW];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-    for (int m = 0; m < NW; ++m)
-#pragma unroll
-      for (int tb = 0; tb < MT; ++tb) acc[nb][m][tb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int m = 0; m < NW; ++m) acc[nb][m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-  const bf16x8 minus24 = splat_bf16(0xC1C0u);   // -(16 + 8)
+  const bf16x8 minus24 = splat_bf16(0xC1C0u), ones = splat_bf16(0x3F80u);   // -(16 + 8); 1
+  const unsigned sixteen = two_sixteens();
   auto multiply = [&](const Stage& st) {
+    bf16x8 xp[kSteps][P];
 #pragma unroll
-    for (int tb = 0; tb < MT; ++tb)
-      if (tb < nblk) {
-        bf16x8 xp[kSteps][P];
+    for (int j = 0; j < kSteps; ++j) st.x[j].parts(xp[j]);
 #pragma unroll
-        for (int j = 0; j < kSteps; ++j) st.x[tb][j].parts(xp[j]);
+    for (int gi = 0; gi < G; ++gi) {
+      f32x4 start = {0.0f, 0.0f, 0.0f, 0.0f};   // -24 * sum x, or with zero points sum x
+      if constexpr (!F32) {
 #pragma unroll
-        for (int gi = 0; gi < G; ++gi) {
-          f32x4 start = {0.0f, 0.0f, 0.0f, 0.0f};
-          if constexpr (!ZERO) {
+        for (int j = gi * kGroupSteps; j < (gi + 1) * kGroupSteps; ++j)
+          start = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xp[j][0], ZERO ? ones : minus24, start, 0, 0, 0);
+      }
 #pragma unroll
-            for (int j = gi * kGroupSteps; j < (gi + 1) * kGroupSteps; ++j)
+      for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-              for (int n = 0; n < P; ++n) start = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xp[j][n], minus24, start, 0, 0, 0);
+        for (int m = 0; m < NW; ++m) {
+          const B& w = st.w[nb][m];
+          f32x4 part = start;
+          if constexpr (ZERO && !F32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) part[e] *= w.minus_zero(gi);
           }
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
+          for (int j = gi * kGroupSteps; j < (gi + 1) * kGroupSteps; ++j) {
+            const bf16x8 v = F32 ? exact_operand_of(w.q[j], sixteen, w.minus_zero(gi)) : operand_of(w.q[j], sixteen);
 #pragma unroll
-            for (int m = 0; m < NW; ++m) {
-              f32x4 part = start;
-              if constexpr (ZERO) {
-                const bf16x8 minus = splat_bf16(st.s[nb][m][gi]);
+            for (int n = 0; n < P; ++n) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xp[j][n], v, part, 0, 0, 0);
+          }
 #pragma unroll
-                for (int j = gi * kGroupSteps; j < (gi + 1) * kGroupSteps; ++j)
-#pragma unroll
-                  for (int n = 0; n < P; ++n) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xp[j][n], minus, part, 0, 0, 0);
-              }
-#pragma unroll
-              for (int j = gi * kGroupSteps; j < (gi + 1) * kGroupSteps; ++j) {
-                const bf16x8 w = operand_of(st.q[nb][m][j]);
-#pragma unroll
-                for (int n = 0; n < P; ++n) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xp[j][n], w, part, 0, 0, 0);
-              }
-              const float scale = __uint_as_float(st.s[nb][m][gi] & 0xFFFF0000u);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) acc[nb][m][tb][e] = fmaf(scale, part[e], acc[nb][m][tb][e]);
-            }
+          for (int e = 0; e < 4; ++e) acc[nb][m][e] = fmaf(w.scale(gi), part[e], acc[nb][m][e]);
         }
-      }
+    }
   };
 
-  const int blocks = a.kblocks * a.mats;
-  const int kb_begin = blocks * wave / 4, kb_end = blocks * (wave + 1) / 4;
-  if (kb_begin < kb_end) {   // wave-uniform
-    Stage s0, s1;
-    load(s0, kb_begin);
-    for (int kb = kb_begin; kb < kb_end; kb += 2) {
-      const bool more1 = kb + 1 < kb_end, more2 = kb + 2 < kb_end;   // past the end the last block is fetched again and not used
-      load(s1, more1 ? kb + 1 : kb);
-      multiply(s0);
-      load(s0, more2 ? kb + 2 : more1 ? kb + 1 : kb);
-      if (more1) multiply(s1);
+  Stage ring[kRing];
+#pragma unroll
+  for (int i = 0; i < kRing - 1; ++i)
+    if (kb_begin + i < kb_end) load(ring[i], kb_begin + i);
+  for (int kb = kb_begin; kb < kb_end;) {   // wave-uniform
+#pragma unroll
+    for (int i = 0; i < kRing; ++i) {
+      if (kb + kRing - 1 < kb_end) load(ring[(i + kRing - 1) % kRing], kb + kRing - 1);
+      multiply(ring[i]);
+      if (++kb == kb_end) break;
     }
   }
 
   // the four waves' sums, added in the order of K; wave e finishes element e of every accumulator
-  __shared__ float s_red[4][NB * NW * MT * 4][64];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
     for (int m = 0; m < NW; ++m)
 #pragma unroll
-      for (int tb = 0; tb < MT; ++tb)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s_red[wave][((nb * NW + m) * MT + tb) * 4 + e][lane] = acc[nb][m][tb][e];
+      for (int e = 0; e < 4; ++e) s_red[wave][(nb * NW + m) * 4 + e][lane] = acc[nb][m][e];
   __syncthreads();
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    float v[NW];
+#pragma unroll
+    for (int m = 0; m < NW; ++m) {
+      const int at = (nb * NW + m) * 4 + wave;
+      v[m] = ((s_red[0][at][lane] + s_red[1][at][lane]) + s_red[2][at][lane]) + s_red[3][at][lane];
+    }
+    const int token = ti.m0 + c * 4 + wave, col = (unit0 + nb) * kUnit + r;
+    if (token < ti.rows && col < a.g.N) {
+      const float y = NW == 2 ? v[0] / (1.0f + expf(-v[0])) * v[NW - 1] : v[0];
+      const size_t at = (size_t)(ti.row_base + token) * a.g.ldc + group_col0(a.g, ti.group) + col;
+      if constexpr (F32) static_cast<float*>(a.g.C)[at] = y;
+      else static_cast<__bf16*>(a.g.C)[at] = (__bf16)y;   // rounded to nearest: the layer's type between the two products
+    }
+  }
+}
+
+template <int NB, int NW, int G, bool ZERO, bool F32>
+__global__ __launch_bounds__(256, 2) void w4_gemm(const Args first, const Args second, const int b_blocks) {
+  __shared__ Place s_place;
+  __shared__ float s_red[4][NB * NW * 4][64];
+  const Place place = find_place<16>(first, second, b_blocks, NB, 16, NB, &s_place);
+  if (place.ti.group < 0) return;
+  split_product<NB, NW, G, ZERO, F32>((int)blockIdx.x < b_blocks ? second : first, place.ti, place.cb * NB, s_red);
+}
+
+// The same product for more rows: the four waves of a workgroup take NB units each over the whole K, and share x: a K block of it
+// is brought to LDS once per workgroup, in whole cache lines, while the block before it is multiplied.  (With K split over the waves, each
+// would read its own quarter of x, row by row: from 8 rows per expert on more bytes than its codes, and 16 cache lines per load.)
+constexpr int kPitch = kBlockK * 2 + 16;   // bytes between rows in LDS: 16 rows' 16-byte pieces fall on different banks
+
+// MB: blocks of 16 rows that are multiplied (of the MT that a row tile may have)
+template <int MB, int NB, int NW, int G, bool ZERO, int kRing>
+__device__ __forceinline__ void tile_product(const Args& a, const TileInfo& ti, int unit0, char* s_x) {
+  constexpr int kSteps = kBlockK / 32, kGroupSteps = kSteps / G;
+  typedef Block<G, ZERO> B;
+  constexpr int kBuffer = 16 * MB * kPitch;
+  const int lane = threadIdx.x & 63;
+  const int r = lane & 15, c = lane >> 4;
+  const int units = (a.g.N + kUnit - 1) / kUnit;
+  const long long matrix = __builtin_amdgcn_readfirstlane(a.g.grp_widx ? a.g.grp_widx[ti.group] : a.g.w_base + ti.group);
+
+  // staging: thread owns 16-byte piece `piece` of rows tid / 16 + 16 * i
+  const int piece = threadIdx.x & 15, row_in = threadIdx.x >> 4;
+  const char* xrow[MB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {
+    int lr = ti.m0 + row_in + 16 * i;
+    if (lr >= ti.rows) lr = ti.rows - 1;   // rows past the group's end repeat its last one; dropped at the end
+    const long long logical = ti.row_base + lr;
+    const long long src = a.g.a_rows ? a.g.a_rows[logical] : logical;
+    xrow[i] = static_cast<const char*>(a.g.A) + src * a.g.lda * 2 + piece * 16;
+  }
+  const int blocks = a.kblocks * a.mats;
+
+  struct Stage {
+    B w[NB][NW];
+    u32x4 x[MB];
+  };
+  // codes and scales: scalar bases that walk the K blocks (and the matrices), and one 32-bit offset per lane
+  const char* code_at[NB];
+  const char* scale_at[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const long long block = (long long)min(unit0 + nb, units - 1) * a.kblocks * NW;   // past the last unit: read it again, dropped
+    code_at[nb] = a.codes + matrix * a.code_stride + block * kBlockBytes;
+    scale_at[nb] = a.scales + matrix * a.scale_stride + block * (kUnit * B::kScaleBytes);
+  }
+  const unsigned lane16 = lane * 16, scale_off = r * B::kScaleBytes;
+  int code_kin = 0;
+  auto load_codes = [&](Stage& st) {   // the next K block's
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+      for (int m = 0; m < NW; ++m)
+        st.w[nb][m].load(code_at[nb] + m * kBlockBytes, scale_at[nb] + m * (kUnit * B::kScaleBytes), lane16, scale_off);
+      code_at[nb] += NW * kBlockBytes;
+      scale_at[nb] += NW * kUnit * B::kScaleBytes;
+    }
+    if (++code_kin == a.kblocks) {   // on to the next matrix
+      code_kin = 0;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        code_at[nb] += a.code_stride - (long long)a.kblocks * NW * kBlockBytes;
+        scale_at[nb] += a.scale_stride - (long long)a.kblocks * NW * kUnit * B::kScaleBytes;
+      }
+    }
+  };
+  int x_kin = 0;
+  auto load_x = [&](Stage& st) {   // the next K block's
+    const bool in = x_kin * kBlockK + piece * 8 < a.g.kseg;
+    const bool wraps = ++x_kin == a.kblocks;
+    const int step = wraps ? (a.g.kseg - (a.kblocks - 1) * kBlockK) * 2 : kBlockK * 2;
+    if (wraps) x_kin = 0;
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+      st.x[i] = u32x4{0, 0, 0, 0};
+      if (in) st.x[i] = *reinterpret_cast<const u32x4*>(xrow[i]);
+      xrow[i] += step;
+    }
+  };
+  auto store_x = [&](const Stage& st, int buf) {
+#pragma unroll
+    for (int i = 0; i < MB; ++i) *reinterpret_cast<u32x4*>(s_x + buf * kBuffer + (row_in + 16 * i) * kPitch + piece * 16) = st.x[i];
+  };
+
+  f32x4 acc[NB][NW][MB];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-    for (int tb = 0; tb < MT; ++tb) {
-      float v[NW];
+    for (int m = 0; m < NW; ++m)
 #pragma unroll
-      for (int m = 0; m < NW; ++m) {
-        const int at = ((nb * NW + m) * MT + tb) * 4 + wave;
-        v[m] = ((s_red[0][at][lane] + s_red[1][at][lane]) + s_red[2][at][lane]) + s_red[3][at][lane];
+      for (int tb = 0; tb < MB; ++tb) acc[nb][m][tb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+  const bf16x8 minus24 = splat_bf16(0xC1C0u), ones = splat_bf16(0x3F80u);   // -(16 + 8); 1
+  const unsigned sixteen = two_sixteens();
+  auto multiply = [&](const Stage& st, int buf) {
+#pragma unroll
+    for (int gi = 0; gi < G; ++gi) {
+      bf16x8 xp[kGroupSteps][MB];
+      f32x4 start[MB];   // -24 * sum x, or with zero points sum x
+#pragma unroll
+      for (int tb = 0; tb < MB; ++tb) {
+        start[tb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < kGroupSteps; ++j) {
+          xp[j][tb] = *reinterpret_cast<const bf16x8*>(s_x + buf * kBuffer + (tb * 16 + r) * kPitch + (gi * kGroupSteps + j) * 64 + c * 16);
+          start[tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xp[j][tb], ZERO ? ones : minus24, start[tb], 0, 0, 0);
+        }
       }
-      const int token = ti.m0 + tb * 16 + c * 4 + wave, col = (unit0 + nb) * kUnit + r;
-      if (token < ti.rows && col < a.g.N) {
-        const float y = NW == 2 ? v[0] / (1.0f + expf(-v[0])) * v[NW - 1] : v[0];
-        const size_t at = (size_t)(ti.row_base + token) * a.g.ldc + group_col0(a.g, ti.group) + col;
-        if constexpr (F32) static_cast<float*>(a.g.C)[at] = y;
-        else static_cast<__bf16*>(a.g.C)[at] = (__bf16)y;   // rounded to nearest: the layer's type between the two products
-      }
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int m = 0; m < NW; ++m) {
+          const B& w = st.w[nb][m];
+          const float scale = w.scale(gi);
+          f32x4 part[MB];
+#pragma unroll
+          for (int tb = 0; tb < MB; ++tb) {
+            part[tb] = start[tb];
+            if constexpr (ZERO) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) part[tb][e] *= w.minus_zero(gi);
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < kGroupSteps; ++j) {
+            const bf16x8 v = operand_of(w.q[gi * kGroupSteps + j], sixteen);
+#pragma unroll
+            for (int tb = 0; tb < MB; ++tb) part[tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xp[j][tb], v, part[tb], 0, 0, 0);
+          }
+#pragma unroll
+          for (int tb = 0; tb < MB; ++tb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[nb][m][tb][e] = fmaf(scale, part[tb][e], acc[nb][m][tb][e]);
+        }
+      if constexpr (G > 1) __builtin_amdgcn_sched_barrier(0);   // or the next groups' x would be read early, and registers spilled
     }
+  };
+
+  // codes and x kRing - 1 K blocks ahead in registers, x one ahead in LDS; one barrier per K block: whoever passes it has read the
+  // buffer that is written next
+  Stage ring[kRing];
+#pragma unroll
+  for (int i = 0; i < kRing - 1; ++i)
+    if (i < blocks) {
+      load_x(ring[i]);
+      load_codes(ring[i]);
+    }
+  store_x(ring[0], 0);
+  __syncthreads();
+  for (int kb = 0; kb < blocks;) {   // uniform over the workgroup
+#pragma unroll
+    for (int i = 0; i < kRing; ++i) {
+      Stage& next = ring[(i + kRing - 1) % kRing];
+      if (kb + kRing - 1 < blocks) {
+        load_x(next);
+        load_codes(next);
+      }
+      multiply(ring[i], i & 1);
+      if (++kb == blocks) break;
+      store_x(ring[(i + 1) % kRing], 1 - (i & 1));
+      __syncthreads();
+    }
+  }
+
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int col = (unit0 + nb) * kUnit + r;
+    if (col >= a.g.N) continue;
+    __bf16* out = static_cast<__bf16*>(a.g.C) + (size_t)ti.row_base * a.g.ldc + group_col0(a.g, ti.group) + col;
+#pragma unroll
+    for (int tb = 0; tb < MB; ++tb)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int token = ti.m0 + tb * 16 + c * 4 + e;
+        const float g = acc[nb][0][tb][e];
+        if (token < ti.rows) out[(size_t)token * a.g.ldc] = (__bf16)(NW == 2 ? g / (1.0f + expf(-g)) * acc[nb][NW - 1][tb][e] : g);
+      }
+  }
+}
+
+// SPLIT: the second problem's workgroups take 16 rows of one unit with K split over the waves, as in w4_gemm.  The shared experts' down
+// projection walks the matrices of all of them: with 4 of them and the whole K to a wave, 44 K blocks one after the other, which took
+// longer than the routed experts' whole product up to 64 tokens (17 tokens, 4 of 60 experts: 26.3 us, split 19.0).
+template <int MT, int NB, int NW, int G, bool ZERO, int kRing, bool SPLIT>
+__global__ __launch_bounds__(256, MT * NB > 2 ? 2 : MT == 2 && NW == 2 && G == 4 ? 3 : 4) void w4_tile_gemm(const Args first, const Args second, const int b_blocks) {
+  constexpr int BM = 16 * MT;
+  static_assert(kRing % 2 == 0, "the LDS buffers alternate");
+  __shared__ Place s_place;
+  __shared__ __attribute__((aligned(16))) char s_x[2 * BM * kPitch];
+  const Place place = find_place<BM>(first, second, b_blocks, 4 * NB, SPLIT ? 16 : BM, SPLIT ? 1 : 4 * NB, &s_place);
+  const TileInfo& ti = place.ti;
+  if (ti.group < 0) return;
+  const bool is_second = (int)blockIdx.x < b_blocks;   // uniform
+  if constexpr (SPLIT) {
+    if (is_second) {
+      static_assert(sizeof(float[4][NW * 4][64]) <= sizeof(s_x), "the sums fit where x would be");
+      split_product<1, NW, G, ZERO, false>(second, ti, place.cb, reinterpret_cast<float (*)[NW * 4][64]>(s_x));
+      return;
+    }
+  }
+  const Args& a = is_second ? second : first;
+  const int unit0 = (place.cb * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * NB;
+  const int left = ti.rows - ti.m0;   // a tile's empty blocks of 16 rows are not multiplied
+  if (MT == 1 || left <= 16) tile_product<1, NB, NW, G, ZERO, kRing>(a, ti, unit0, s_x);
+  else if (MT == 2 || left <= 32) tile_product<(MT < 2 ? MT : 2), NB, NW, G, ZERO, kRing>(a, ti, unit0, s_x);
+  else tile_product<MT, NB, NW, G, ZERO, kRing>(a, ti, unit0, s_x);
 }
 
 // ---- quantisation, values, packing ----------------------------------------------------------------------------------------
@@ -452,42 +731,61 @@ static int grid_for(long long threads) {
   return (int)(blocks < 16384 ? blocks : 16384);
 }
 
-template <int MT, int NB, int NW, bool F32>
+// TILE: w4_tile_gemm, whose workgroups have 4 * NB units (SPLIT: of the second problem one); else w4_gemm with NB
+template <bool TILE, int MT, int NB, int NW, bool F32, int RING, bool SPLIT = false>
 static int launch_typed(const Args& a, const Args* b, int group, bool zeros, int total_rows, hipStream_t s) {
-  constexpr int BM = 16 * MT;
-  const int n_cb = ((a.g.N + kUnit - 1) / kUnit + NB - 1) / NB;
+  constexpr int BM = 16 * MT, UNITS = TILE ? 4 * NB : NB, B_ROWS = SPLIT ? 16 : BM, B_UNITS = SPLIT ? 1 : UNITS;
+  const int n_cb = ((a.g.N + kUnit - 1) / kUnit + UNITS - 1) / UNITS;
   // row tiles of the grouped rows: at most one partly filled one per group, and none without a row
   long long m_tiles = ((long long)total_rows + (long long)a.g.ngroups * (BM - 1)) / BM;
   if (m_tiles > total_rows) m_tiles = total_rows;
-  const long long a_blocks = m_tiles * n_cb;
-  long long grid = a_blocks;
-  if (b) grid += (b->g.ngroups * (long long)n_cb + 7) / 8 * 8 * ((b->g.M + BM - 1) / BM);
-  if (grid == 0) return OCCULT_OK;
+  const long long a_blocks = m_tiles * ((n_cb + 7) / 8) * 8;   // an XCD has at most ceil(n_cb / 8) column blocks of a group
+  const int b_cb = ((a.g.N + kUnit - 1) / kUnit + B_UNITS - 1) / B_UNITS;
+  const long long b_blocks = b ? (b->g.ngroups * (long long)b_cb + 7) / 8 * 8 * ((b->g.M + B_ROWS - 1) / B_ROWS) : 0;
+  const long long grid = a_blocks + b_blocks;
   OCC_REQUIRE(grid < (1ll << 24), OCCULT_ESHAPE, "%lld workgroups are too many for one launch", grid);
   const Args& second = b ? *b : a;
 #define OCC_W4_CASE(G_, Z_)                                                                                                \
   if (group == kBlockK / G_ && zeros == Z_) {                                                                              \
-    w4_gemm<MT, NB, NW, G_, Z_, F32><<<(int)grid, 256, 0, s>>>(a, second, (int)a_blocks);                                  \
-    OCC_LAUNCH_CHECK("w4_gemm");                                                                                           \
+    if constexpr (TILE) w4_tile_gemm<MT, NB, NW, G_, Z_, RING, SPLIT><<<(int)grid, 256, 0, s>>>(a, second, (int)b_blocks);        \
+    else w4_gemm<NB, NW, G_, Z_, F32><<<(int)grid, 256, 0, s>>>(a, second, (int)b_blocks);                                 \
+    OCC_LAUNCH_CHECK(TILE ? "w4_tile_gemm" : "w4_gemm");                                                                   \
     return OCCULT_OK;                                                                                                      \
   }
   OCC_W4_CASE(1, false)
-  OCC_W4_CASE(2, false)
   OCC_W4_CASE(4, false)
-  OCC_W4_CASE(1, true)
   OCC_W4_CASE(2, true)
+  OCC_W4_CASE(2, false)
+  OCC_W4_CASE(1, true)
   OCC_W4_CASE(4, true)
 #undef OCC_W4_CASE
   OCC_FAIL(OCCULT_EINVAL, "group=%d", group);
 }
 
-// a: the routed experts' grouped rows; b: the shared experts', or NULL
+// a: the routed experts' grouped rows; b: the shared experts', or NULL.  Times below: gate/up or down product of the layers with 60 (4 per
+// token, 4 shared) and 64 experts (8 per token), K = 2048 and 1408 or 1024.
 template <int NW>
 static int launch(const occult_cfg_t& c, const Args& a, const Args* b, int group, bool zeros, hipStream_t s) {
   const int rows = c.T * c.k;
-  if (c.dtype == OCCULT_F32) return launch_typed<1, 2, NW, true>(a, b, group, zeros, rows, s);
-  if (rows <= 8ll * c.E) return launch_typed<1, 2, NW, false>(a, b, group, zeros, rows, s);
-  return launch_typed<2, 2, NW, false>(a, b, group, zeros, rows, s);
+  if (c.dtype == OCCULT_F32) return launch_typed<false, 1, 2, NW, true, 2>(a, b, group, zeros, rows, s);
+  // K split over the waves while whole-K workgroups would not fill the chip one and a half times: 1 token, gate/up 7.7 against
+  // 11.0 us (60 experts) and 7.2 against 12.5 (64), 2 tokens 11.3 against 15.0 (64: 256 workgroups); 4 tokens 16.3 against 15.0 (60: 440)
+  const long long tiles = min_i(rows, rows / 16 + c.E) + (b ? (long long)b->g.ngroups * ((c.T + 15) / 16) : 0);
+  if (tiles * ((a.g.N + 4 * kUnit - 1) / (4 * kUnit)) <= 384) return launch_typed<false, 1, NW == 2 ? 1 : 2, NW, false, 2>(a, b, group, zeros, rows, s);
+  const long long per_expert = rows / c.E;
+  if constexpr (NW == 1) {
+    // a long sum over the shared experts' matrices beside short routed ones: 17 tokens, 60 experts, 19.0 against 26.3 us; 32 tokens 22.2
+    // against 27.5; 64 tokens 28.9 against 27.8; with 2 shared experts no gain (17 tokens 20.8 against 20.3)
+    if (b && b->mats * b->kblocks >= 32 && c.T <= 48) return launch_typed<true, 1, 1, 1, false, 4, true>(a, b, group, zeros, rows, s);
+    // 32 columns per wave halve the reads of x; fewer workgroups: 250 tokens, 64 experts (23 rows per expert) 33.0 against 37.8 us, 60
+    // experts (16 rows) 42.2 against 37.1
+    if (per_expert >= 20) return launch_typed<true, 2, 2, 1, false, 2>(a, b, group, zeros, rows, s);
+  }
+  // 32-row tiles decode an expert's codes once for up to 32 rows, in a third more registers: gate/up, 60 experts, 4 rows per expert 36.8
+  // against 34.0 us, 8 rows 40.4 against 41.6, 16 rows 53.7 against 62.2; with groups of 32, whose scaling takes registers too, 8 rows
+  // 54.7 against 51.3, 12 rows 54.7 against 52.4, 16 rows 68.9 against 76.3
+  if (per_expert >= (NW == 2 && group == 32 ? 14 : 6)) return launch_typed<true, 2, 1, NW, false, 2>(a, b, group, zeros, rows, s);
+  return launch_typed<true, 1, 1, NW, false, 2>(a, b, group, zeros, rows, s);
 }
 
 }  // namespace w4
