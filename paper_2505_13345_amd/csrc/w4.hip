@@ -172,6 +172,17 @@ struct XFrag<true> {
   }
 };
 
+// Sum over this and the lower lanes: shifts inside rows of 16 lanes, then a row's last lane to the next row, then lane 31 to the upper half
+__device__ __forceinline__ int wave_prefix_sum(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);   // row_shr:1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast:15, rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // row_bcast:31, rows 2 and 3
+  return v;
+}
+
 // Row tile and column block of a workgroup.  Workgroups [0, b_blocks) work on the second problem (the shared experts, whose down
 // projection has the longest K: they start first), the rest on the first.  The row tiles that read the same weights get ids 8
 // apart: they run on the same XCD, at about the same time, and all but the first find the codes in its L2 (500 tokens, 6 of 64 experts:
@@ -181,7 +192,7 @@ struct XFrag<true> {
 // group = -1: nothing to do.  Called by the whole workgroup, whose first wave does the work.
 struct Place {
   TileInfo ti;
-  int cb;
+  int cb, matrix;                    // column block; weight matrix
 };
 template <int BM>
 __device__ __forceinline__ Place find_place(const Args& first, const Args& second, int b_blocks, int units_per_block, int b_rows,
@@ -193,7 +204,7 @@ __device__ __forceinline__ Place find_place(const Args& first, const Args& secon
     const int n_cb = ((g.N + kUnit - 1) / kUnit + per_block - 1) / per_block;
     Place p;
     p.ti.group = -1;
-    p.ti.m0 = p.ti.rows = p.ti.row_base = p.cb = 0;
+    p.ti.m0 = p.ti.rows = p.ti.row_base = p.cb = p.matrix = 0;
     if (bid < b_blocks) {
       const int tiles = (g.M + b_rows - 1) / b_rows;
       const int unit = bid / (8 * tiles) * 8 + (bid & 7);
@@ -202,6 +213,7 @@ __device__ __forceinline__ Place find_place(const Args& first, const Args& secon
         p.ti.m0 = (bid >> 3) % tiles * b_rows;
         p.ti.rows = g.M;
         p.cb = unit % n_cb;
+        p.matrix = g.w_base + p.ti.group;
       }
       if (lane == 0) *s_place = p;
     } else {
@@ -211,15 +223,11 @@ __device__ __forceinline__ Place find_place(const Args& first, const Args& secon
       for (int c0 = 0; c0 < g.ngroups; c0 += 64) {
         const int group = c0 + lane;
         const int lo = group < g.ngroups ? g.grp_offset[group] : 0, hi = group < g.ngroups ? g.grp_offset[group + 1] : 0;
+        const int matrix = group < g.ngroups ? g.grp_widx[group] : 0;   // beside the offsets: the codes' addresses wait for it
         const int tiles = (hi - lo + BM - 1) / BM;
         const int cb0 = (xcd - group * n_cb) & 7;   // this group's first column block on this XCD
         const int mine = cb0 < n_cb ? (n_cb - cb0 + 7) / 8 : 0;
-        int incl = tiles * mine;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-          const int v = __shfl_up(incl, o, 64);
-          if (lane >= o) incl += v;
-        }
+        const int incl = wave_prefix_sum(tiles * mine);
         const int excl = before + incl - tiles * mine;
         if (at >= excl && at < excl + tiles * mine) {   // at most one lane over all chunks
           p.ti.group = group;
@@ -227,9 +235,10 @@ __device__ __forceinline__ Place find_place(const Args& first, const Args& secon
           p.ti.rows = hi - lo;
           p.ti.row_base = lo;
           p.cb = cb0 + (at - excl) / tiles * 8;
+          p.matrix = matrix;
           *s_place = p;
         }
-        before += __shfl(incl, 63, 64);
+        before += __builtin_amdgcn_readlane(incl, 63);
         if (before > at) break;   // uniform
       }
     }
@@ -241,6 +250,7 @@ __device__ __forceinline__ Place find_place(const Args& first, const Args& secon
   p.ti.rows = __builtin_amdgcn_readfirstlane(p.ti.rows);
   p.ti.row_base = __builtin_amdgcn_readfirstlane(p.ti.row_base);
   p.cb = __builtin_amdgcn_readfirstlane(p.cb);
+  p.matrix = __builtin_amdgcn_readfirstlane(p.matrix);
   return p;
 }
 
@@ -248,7 +258,7 @@ __device__ __forceinline__ Place find_place(const Args& first, const Args& secon
 // to 16 rows of one group, and add their sums through LDS in the order of K.  For few rows, where the length of a wave's stream is
 // what counts: every wave has kRing - 1 K blocks in flight.
 template <int NB, int NW, int G, bool ZERO, bool F32>
-__device__ __forceinline__ void split_product(const Args& a, const TileInfo& ti, int unit0, float (*s_red)[NB * NW * 4][64]) {
+__device__ __forceinline__ void split_product(const Args& a, const TileInfo& ti, long long matrix, int unit0, float (*s_red)[NB * NW * 4][64]) {
   constexpr int kSteps = kBlockK / 32, kGroupSteps = kSteps / G;
   constexpr int P = XFrag<F32>::kParts;
   constexpr int kRing = F32 ? 2 : 4;
@@ -256,7 +266,6 @@ __device__ __forceinline__ void split_product(const Args& a, const TileInfo& ti,
   const int units = (a.g.N + kUnit - 1) / kUnit;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, c = lane >> 4;
-  const long long matrix = __builtin_amdgcn_readfirstlane(a.g.grp_widx ? a.g.grp_widx[ti.group] : a.g.w_base + ti.group);
   // this wave's K blocks, counted through the matrices that K walks
   const int blocks = a.kblocks * a.mats;
   const int kb_begin = blocks * wave / 4, kb_end = blocks * (wave + 1) / 4;
@@ -377,7 +386,7 @@ __global__ __launch_bounds__(256, 2) void w4_gemm(const Args first, const Args s
   __shared__ float s_red[4][NB * NW * 4][64];
   const Place place = find_place<16>(first, second, b_blocks, NB, 16, NB, &s_place);
   if (place.ti.group < 0) return;
-  split_product<NB, NW, G, ZERO, F32>((int)blockIdx.x < b_blocks ? second : first, place.ti, place.cb * NB, s_red);
+  split_product<NB, NW, G, ZERO, F32>((int)blockIdx.x < b_blocks ? second : first, place.ti, place.matrix, place.cb * NB, s_red);
 }
 
 // The same product for more rows: the four waves of a workgroup take NB units each over the whole K, and share x: a K block of it
@@ -387,26 +396,25 @@ constexpr int kPitch = kBlockK * 2 + 16;   // bytes between rows in LDS: 16 rows
 
 // MB: blocks of 16 rows that are multiplied (of the MT that a row tile may have)
 template <int MB, int NB, int NW, int G, bool ZERO, int kRing>
-__device__ __forceinline__ void tile_product(const Args& a, const TileInfo& ti, int unit0, char* s_x) {
+__device__ __forceinline__ void tile_product(const Args& a, const TileInfo& ti, long long matrix, int unit0, char* s_x) {
   constexpr int kSteps = kBlockK / 32, kGroupSteps = kSteps / G;
   typedef Block<G, ZERO> B;
   constexpr int kBuffer = 16 * MB * kPitch;
   const int lane = threadIdx.x & 63;
   const int r = lane & 15, c = lane >> 4;
   const int units = (a.g.N + kUnit - 1) / kUnit;
-  const long long matrix = __builtin_amdgcn_readfirstlane(a.g.grp_widx ? a.g.grp_widx[ti.group] : a.g.w_base + ti.group);
 
   // staging: thread owns 16-byte piece `piece` of rows tid / 16 + 16 * i
   const int piece = threadIdx.x & 15, row_in = threadIdx.x >> 4;
-  const char* xrow[MB];
+  int src[MB];
 #pragma unroll
-  for (int i = 0; i < MB; ++i) {
-    int lr = ti.m0 + row_in + 16 * i;
-    if (lr >= ti.rows) lr = ti.rows - 1;   // rows past the group's end repeat its last one; dropped at the end
-    const long long logical = ti.row_base + lr;
-    const long long src = a.g.a_rows ? a.g.a_rows[logical] : logical;
-    xrow[i] = static_cast<const char*>(a.g.A) + src * a.g.lda * 2 + piece * 16;
+  for (int i = 0; i < MB; ++i)   // rows past the group's end repeat its last one; dropped at the end
+    src[i] = ti.row_base + min(ti.m0 + row_in + 16 * i, ti.rows - 1);
+  if (a.g.a_rows) {
+#pragma unroll
+    for (int i = 0; i < MB; ++i) src[i] = a.g.a_rows[src[i]];
   }
+  const char* xrow[MB];   // set below, when the first codes have been asked for
   const int blocks = a.kblocks * a.mats;
 
   struct Stage {
@@ -427,13 +435,15 @@ __device__ __forceinline__ void tile_product(const Args& a, const TileInfo& ti, 
   auto load_codes = [&](Stage& st) {   // the next K block's
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
+      // held in scalar registers: the compiler would carry base plus lane offset along per lane, a 64-bit addition for every load
+      asm volatile("" : "+s"(code_at[nb]), "+s"(scale_at[nb]));
 #pragma unroll
       for (int m = 0; m < NW; ++m)
         st.w[nb][m].load(code_at[nb] + m * kBlockBytes, scale_at[nb] + m * (kUnit * B::kScaleBytes), lane16, scale_off);
       code_at[nb] += NW * kBlockBytes;
       scale_at[nb] += NW * kUnit * B::kScaleBytes;
     }
-    if (++code_kin == a.kblocks) {   // on to the next matrix
+    if (NW == 1 && ++code_kin == a.kblocks) {   // on to the next matrix (gate and up have one)
       code_kin = 0;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
@@ -445,7 +455,7 @@ __device__ __forceinline__ void tile_product(const Args& a, const TileInfo& ti, 
   int x_kin = 0;
   auto load_x = [&](Stage& st) {   // the next K block's
     const bool in = x_kin * kBlockK + piece * 8 < a.g.kseg;
-    const bool wraps = ++x_kin == a.kblocks;
+    const bool wraps = ++x_kin == a.kblocks && NW == 1;
     const int step = wraps ? (a.g.kseg - (a.kblocks - 1) * kBlockK) * 2 : kBlockK * 2;
     if (wraps) x_kin = 0;
 #pragma unroll
@@ -519,10 +529,12 @@ __device__ __forceinline__ void tile_product(const Args& a, const TileInfo& ti, 
   Stage ring[kRing];
 #pragma unroll
   for (int i = 0; i < kRing - 1; ++i)
-    if (i < blocks) {
-      load_x(ring[i]);
-      load_codes(ring[i]);
-    }
+    if (i < blocks) load_codes(ring[i]);   // before x, whose addresses wait for the row indices
+#pragma unroll
+  for (int i = 0; i < MB; ++i) xrow[i] = static_cast<const char*>(a.g.A) + (long long)src[i] * a.g.lda * 2 + piece * 16;
+#pragma unroll
+  for (int i = 0; i < kRing - 1; ++i)
+    if (i < blocks) load_x(ring[i]);
   store_x(ring[0], 0);
   __syncthreads();
   for (int kb = 0; kb < blocks;) {   // uniform over the workgroup
@@ -560,7 +572,7 @@ __device__ __forceinline__ void tile_product(const Args& a, const TileInfo& ti, 
 // projection walks the matrices of all of them: with 4 of them and the whole K to a wave, 44 K blocks one after the other, which took
 // longer than the routed experts' whole product up to 64 tokens (17 tokens, 4 of 60 experts: 26.3 us, split 19.0).
 template <int MT, int NB, int NW, int G, bool ZERO, int kRing, bool SPLIT>
-__global__ __launch_bounds__(256, MT * NB > 2 ? 2 : MT == 2 && NW == 2 && G == 4 ? 3 : 4) void w4_tile_gemm(const Args first, const Args second, const int b_blocks) {
+__global__ __launch_bounds__(256, MT * NB > 2 ? 2 : MT == 2 && NW == 2 && (G == 4 || !ZERO) ? 3 : MT == 1 && !SPLIT && !(G == 4 && ZERO) ? 5 : 4) void w4_tile_gemm(const Args first, const Args second, const int b_blocks) {
   constexpr int BM = 16 * MT;
   static_assert(kRing % 2 == 0, "the LDS buffers alternate");
   __shared__ Place s_place;
@@ -572,16 +584,16 @@ __global__ __launch_bounds__(256, MT * NB > 2 ? 2 : MT == 2 && NW == 2 && G == 4
   if constexpr (SPLIT) {
     if (is_second) {
       static_assert(sizeof(float[4][NW * 4][64]) <= sizeof(s_x), "the sums fit where x would be");
-      split_product<1, NW, G, ZERO, false>(second, ti, place.cb, reinterpret_cast<float (*)[NW * 4][64]>(s_x));
+      split_product<1, NW, G, ZERO, false>(second, ti, place.matrix, place.cb, reinterpret_cast<float (*)[NW * 4][64]>(s_x));
       return;
     }
   }
   const Args& a = is_second ? second : first;
   const int unit0 = (place.cb * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * NB;
   const int left = ti.rows - ti.m0;   // a tile's empty blocks of 16 rows are not multiplied
-  if (MT == 1 || left <= 16) tile_product<1, NB, NW, G, ZERO, kRing>(a, ti, unit0, s_x);
-  else if (MT == 2 || left <= 32) tile_product<(MT < 2 ? MT : 2), NB, NW, G, ZERO, kRing>(a, ti, unit0, s_x);
-  else tile_product<MT, NB, NW, G, ZERO, kRing>(a, ti, unit0, s_x);
+  if (MT == 1 || left <= 16) tile_product<1, NB, NW, G, ZERO, kRing>(a, ti, place.matrix, unit0, s_x);
+  else if (MT == 2 || left <= 32) tile_product<(MT < 2 ? MT : 2), NB, NW, G, ZERO, kRing>(a, ti, place.matrix, unit0, s_x);
+  else tile_product<MT, NB, NW, G, ZERO, kRing>(a, ti, place.matrix, unit0, s_x);
 }
 
 // ---- quantisation, values, packing ----------------------------------------------------------------------------------------
@@ -768,23 +780,26 @@ template <int NW>
 static int launch(const occult_cfg_t& c, const Args& a, const Args* b, int group, bool zeros, hipStream_t s) {
   const int rows = c.T * c.k;
   if (c.dtype == OCCULT_F32) return launch_typed<false, 1, 2, NW, true, 2>(a, b, group, zeros, rows, s);
-  // K split over the waves while whole-K workgroups would not fill the chip one and a half times: 1 token, gate/up 7.7 against
-  // 11.0 us (60 experts) and 7.2 against 12.5 (64), 2 tokens 11.3 against 15.0 (64: 256 workgroups); 4 tokens 16.3 against 15.0 (60: 440)
+  // K split over the waves while whole-K workgroups would not fill the chip one and a half times: 1 token, gate/up 9.1 against
+  // 12.2 us (60 experts), 2 tokens 12.6 against 14.7 (64: 256 workgroups); 4 tokens 16.1 against 14.3 (60: 440)
   const long long tiles = min_i(rows, rows / 16 + c.E) + (b ? (long long)b->g.ngroups * ((c.T + 15) / 16) : 0);
   if (tiles * ((a.g.N + 4 * kUnit - 1) / (4 * kUnit)) <= 384) return launch_typed<false, 1, NW == 2 ? 1 : 2, NW, false, 2>(a, b, group, zeros, rows, s);
   const long long per_expert = rows / c.E;
   if constexpr (NW == 1) {
-    // a long sum over the shared experts' matrices beside short routed ones: 17 tokens, 60 experts, 19.0 against 26.3 us; 32 tokens 22.2
-    // against 27.5; 64 tokens 28.9 against 27.8; with 2 shared experts no gain (17 tokens 20.8 against 20.3)
-    if (b && b->mats * b->kblocks >= 32 && c.T <= 48) return launch_typed<true, 1, 1, 1, false, 4, true>(a, b, group, zeros, rows, s);
-    // 32 columns per wave halve the reads of x; fewer workgroups: 250 tokens, 64 experts (23 rows per expert) 33.0 against 37.8 us, 60
-    // experts (16 rows) 42.2 against 37.1
-    if (per_expert >= 20) return launch_typed<true, 2, 2, 1, false, 2>(a, b, group, zeros, rows, s);
+    // A long sum over the shared experts' matrices beside short routed ones (4 shared experts: 44 K blocks): 17 tokens split 20.1 against
+    // 25.8 us; 64 tokens split 33.0, codes three blocks ahead 27.8, one ahead 32.2; 128 tokens 33.9 against 38.1.  With 2 or none shared
+    // nothing is gained (64 experts, 17 tokens 18.8 against 16.6).
+    if (b && b->mats * b->kblocks >= 32) {
+      if (c.T <= 48) return launch_typed<true, 1, 1, 1, false, 4, true>(a, b, group, zeros, rows, s);
+      if (per_expert < 12) return launch_typed<true, 1, 1, 1, false, 4>(a, b, group, zeros, rows, s);
+    }
   }
-  // 32-row tiles decode an expert's codes once for up to 32 rows, in a third more registers: gate/up, 60 experts, 4 rows per expert 36.8
-  // against 34.0 us, 8 rows 40.4 against 41.6, 16 rows 53.7 against 62.2; with groups of 32, whose scaling takes registers too, 8 rows
-  // 54.7 against 51.3, 12 rows 54.7 against 52.4, 16 rows 68.9 against 76.3
-  if (per_expert >= (NW == 2 && group == 32 ? 14 : 6)) return launch_typed<true, 2, 1, NW, false, 2>(a, b, group, zeros, rows, s);
+  // Tiles of 32 rows decode an expert's codes half as often as tiles of 16, and with two units per wave x is read half as often; both take
+  // registers, and so waves that hide latency.  Gate/up, us, 16 rows | 32 rows | 32 rows and two units: 8 rows per expert 50.2 | 55.3 | 52.6;
+  // 16 rows 69.4 | 67.4 | 72.2; 23 rows 72.4 | 66.9 | 64.6; 46 rows 116 | 106 | 98; with groups of 32 (four scalings per block)
+  // 23 rows 78.4 | 72.8 | 83.3, 46 rows 131 | 117 | 133.  Down product: 46 rows 81 | 74 | 60.
+  if (per_expert >= 20 && (NW == 1 || group != 32)) return launch_typed<true, 2, 2, NW, false, 2>(a, b, group, zeros, rows, s);
+  if (per_expert >= 16) return launch_typed<true, 2, 1, NW, false, 2>(a, b, group, zeros, rows, s);
   return launch_typed<true, 1, 1, NW, false, 2>(a, b, group, zeros, rows, s);
 }
 
