@@ -15,13 +15,15 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 namespace occult {
 
 namespace norm {
 
 constexpr int kMaxRowBytes = 32768;
 constexpr int kColSums = 5;          // post weight, post bias, pre weight, pre bias, channel gate
-constexpr int kBackwardBlocks = 512; // workgroups of the backward pass that keep column sums, at most
+constexpr int kBackwardBlocks = 256; // workgroups of the backward pass that keep column sums, at most
 
 struct Args {
   const void *x, *y, *gate, *post_w, *post_b, *pre_w, *pre_b;
@@ -40,12 +42,13 @@ struct BackwardArgs {
   float x_scale, y_scale, post_eps, pre_eps, offset, inv_d;
 };
 
-constexpr int block_waves(int W) { return W <= 4 ? 4 : W; }
+// waves of a workgroup: at least 4 in the forward pass; 8 in the backward pass, whose workgroups each leave a set of column sums
+constexpr int block_waves(int W, bool backward) { return backward ? (W <= 8 ? 8 : W) : (W <= 4 ? 4 : W); }
 
-// Which lanes hold which rows.  V vectors per lane, W waves per row; workgroups of 4 waves, or of W.
-template <int V, int W>
+// Which lanes hold which rows.  V vectors per lane, W waves per row.
+template <int V, int W, bool BACKWARD>
 struct Place {
-  static constexpr int kWaves = block_waves(W);
+  static constexpr int kWaves = block_waves(W, BACKWARD);
   int row, lane, stride;             // row inside the workgroup, lane inside the row, lanes of the row
   __device__ Place(int lanes) {
     const int wave = threadIdx.x >> 6, l = threadIdx.x & 63;
@@ -62,20 +65,34 @@ struct Place {
   __device__ static int rows_per_block(int lanes) { return W == 1 ? kWaves * (64 / lanes) : kWaves / W; }
 };
 
+// Sum over aligned groups of `lanes` lanes (a power of two), in each of them.  Inside 16 lanes by DPP operands (neighbours, pairs, then
+// mirrored halves and rows, whose partners hold the sum of the other half), beyond them from a row's lane; a lane exchange
+// through LDS takes longer than all four additions.
+__device__ __forceinline__ float group_sum(float v, int lanes) {
+  auto add = [&](auto ctrl) {
+    const int o = __builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, true);
+    v += __int_as_float(o);
+  };
+  if (lanes >= 2) add(std::integral_constant<int, 0xB1>{});    // quad_perm [1,0,3,2]
+  if (lanes >= 4) add(std::integral_constant<int, 0x4E>{});    // quad_perm [2,3,0,1]
+  if (lanes >= 8) add(std::integral_constant<int, 0x141>{});   // row_half_mirror
+  if (lanes >= 16) add(std::integral_constant<int, 0x140>{});  // row_mirror
+  if (lanes == 32) v += __shfl_xor(v, 16, 64);
+  if (lanes == 64) {
+    const auto row = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); };
+    v = (row(0) + row(16)) + (row(32) + row(48));
+  }
+  return v;
+}
+
 // The sums of N values over the lanes of a row, in every lane.  `slot`: alternates between two LDS areas, so that one barrier per
 // exchange is enough.
-template <int W, int N>
+template <int W, int WAVES, int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], int lanes, int& slot) {
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    if (W > 1 || o < lanes) {
-#pragma unroll
-      for (int n = 0; n < N; ++n) v[n] += __shfl_xor(v[n], o, 64);
-    }
-  }
+  for (int n = 0; n < N; ++n) v[n] = group_sum(v[n], W > 1 ? 64 : lanes);
   if constexpr (W > 1) {
-    constexpr int kWaves = block_waves(W);
-    __shared__ float s_sum[2][N][kWaves];
+    __shared__ float s_sum[2][N][WAVES];
     const int wave = threadIdx.x >> 6, first = wave / W * W;
     if ((threadIdx.x & 63) == 0) {
 #pragma unroll
@@ -137,11 +154,12 @@ __device__ __forceinline__ void weight_of(bool has, float offset, float* w) {
 }
 
 template <bool BF16, int V, int W>
-__global__ __launch_bounds__(64 * block_waves(W)) void block_norm_kernel(const Args a) {
+__global__ __launch_bounds__(64 * block_waves(W, false)) void block_norm_kernel(const Args a) {
   using R = Row<BF16>;
   constexpr int NE = R::kElems;
-  const Place<V, W> p(a.lanes);
-  const int rows = Place<V, W>::rows_per_block(a.lanes);
+  typedef Place<V, W, false> P;
+  const P p(a.lanes);
+  const int rows = P::rows_per_block(a.lanes);
   int slot = 0;
 
   RowRegs<BF16, V> post_w, post_b, pre_w, pre_b, cgate;
@@ -182,7 +200,7 @@ __global__ __launch_bounds__(64 * block_waves(W)) void block_norm_kernel(const A
           for (int i = 0; i < V; ++i)
 #pragma unroll
             for (int e = 0; e < NE; ++e) sum[0] += z[i][e];
-          row_sums<W>(sum, a.lanes, slot);
+          row_sums<W, P::kWaves>(sum, a.lanes, slot);
           mu = sum[0] * a.inv_d;
         }
         float sq[1] = {0.0f};
@@ -195,7 +213,7 @@ __global__ __launch_bounds__(64 * block_waves(W)) void block_norm_kernel(const A
             sq[0] = fmaf(z[i][e], z[i][e], sq[0]);
           }
         }
-        row_sums<W>(sq, a.lanes, slot);
+        row_sums<W, P::kWaves>(sq, a.lanes, slot);
         const float r = 1.0f / sqrtf(fmaf(sq[0], a.inv_d, a.post_eps));
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -232,7 +250,7 @@ __global__ __launch_bounds__(64 * block_waves(W)) void block_norm_kernel(const A
 #pragma unroll
           for (int e = 0; e < NE; ++e) sum[0] += in ? s[i][e] : 0.0f;
         }
-        row_sums<W>(sum, a.lanes, slot);
+        row_sums<W, P::kWaves>(sum, a.lanes, slot);
         mu = sum[0] * a.inv_d;
       }
       float sq[1] = {0.0f};
@@ -245,7 +263,7 @@ __global__ __launch_bounds__(64 * block_waves(W)) void block_norm_kernel(const A
           sq[0] = fmaf(s[i][e], s[i][e], sq[0]);
         }
       }
-      row_sums<W>(sq, a.lanes, slot);
+      row_sums<W, P::kWaves>(sq, a.lanes, slot);
       const float r = 1.0f / sqrtf(fmaf(sq[0], a.inv_d, a.pre_eps));
 #pragma unroll
       for (int i = 0; i < V; ++i) {
@@ -266,14 +284,15 @@ __global__ __launch_bounds__(64 * block_waves(W)) void block_norm_kernel(const A
 // its workgroup in registers, the workgroup's row groups are added through LDS in their order, and the workgroups' sums go to ws, where
 // column_sums_kernel adds them in order: no atomics, the same bits every time.
 template <bool BF16, int V, int W, bool LAYER>
-__global__ __launch_bounds__(64 * block_waves(W)) void block_norm_backward_kernel(const BackwardArgs a) {
+__global__ __launch_bounds__(64 * block_waves(W, true)) void block_norm_backward_kernel(const BackwardArgs a) {
   using R = Row<BF16>;
   constexpr int NE = R::kElems;
   // without a mean-subtracting norm or a bias there are three column sums: weights and gate
   constexpr int NS = LAYER ? kColSums : 3;
   constexpr int kPostW = 0, kPreW = 1, kGate = 2, kPostB = LAYER ? 3 : 0, kPreB = LAYER ? 4 : 0;
-  const Place<V, W> p(a.lanes);
-  const int rows = Place<V, W>::rows_per_block(a.lanes);
+  typedef Place<V, W, true> P;
+  const P p(a.lanes);
+  const int rows = P::rows_per_block(a.lanes);
   int slot = 0;
 
   RowRegs<BF16, V> post_w, post_b, pre_w, cgate;
@@ -291,21 +310,35 @@ __global__ __launch_bounds__(64 * block_waves(W)) void block_norm_backward_kerne
 #pragma unroll
       for (int e = 0; e < NE; ++e) col[n][i][e] = 0.0f;
 
-  for (long long t0 = (long long)blockIdx.x * rows; t0 < a.T; t0 += (long long)gridDim.x * rows) {
+  struct Rows {
+    RowRegs<BF16, V> y, out, dout, dh, gate;
+    float token_gate;
+  };
+  auto load = [&](Rows& r, long long t0) {
+    const bool valid = t0 + p.row < a.T;
+    const size_t t = valid ? t0 + p.row : 0;
+    r.dout.load(a.dout, t, a.row_vecs, p.lane, p.stride, valid && a.dout);
+    r.out.load(a.out, t, a.row_vecs, p.lane, p.stride, valid && a.pre);
+    r.dh.load(a.dh, t, a.row_vecs, p.lane, p.stride, valid && a.pre);
+    r.y.load(a.y, t, a.row_vecs, p.lane, p.stride, valid && need_y);
+    r.gate.load(a.gate, t, a.row_vecs, p.lane, p.stride, valid && a.gate_kind == OCCULT_GATE_ELEMENT);
+    r.token_gate = 1.0f;
+    if (a.gate_kind == OCCULT_GATE_TOKEN) r.token_gate = load_scalar<BF16>(a.gate, t);
+  };
+  const long long step = (long long)gridDim.x * rows;
+  Rows next;
+  load(next, (long long)blockIdx.x * rows);
+  for (long long t0 = (long long)blockIdx.x * rows; t0 < a.T; t0 += step) {
     const bool valid = t0 + p.row < a.T;
     const size_t t = valid ? t0 + p.row : 0;
     post_w.keep_raw();
     post_b.keep_raw();
     pre_w.keep_raw();
     cgate.keep_raw();
-    RowRegs<BF16, V> yr, outr, doutr, dhr, gr;
-    doutr.load(a.dout, t, a.row_vecs, p.lane, p.stride, valid && a.dout);
-    outr.load(a.out, t, a.row_vecs, p.lane, p.stride, valid && a.pre);
-    dhr.load(a.dh, t, a.row_vecs, p.lane, p.stride, valid && a.pre);
-    yr.load(a.y, t, a.row_vecs, p.lane, p.stride, valid && need_y);
-    gr.load(a.gate, t, a.row_vecs, p.lane, p.stride, valid && a.gate_kind == OCCULT_GATE_ELEMENT);
-    float token_gate = 1.0f;
-    if (a.gate_kind == OCCULT_GATE_TOKEN) token_gate = load_scalar<BF16>(a.gate, t);
+    const Rows cur = next;
+    if (t0 + step < a.T) load(next, t0 + step);   // requested before this pass's sums, whose exchanges would otherwise leave memory idle
+    const RowRegs<BF16, V>&yr = cur.y, &outr = cur.out, &doutr = cur.dout, &dhr = cur.dh, &gr = cur.gate;
+    const float token_gate = cur.token_gate;
 
     float D[V][NE], o[V][NE], y[V][NE];   // gradient of the stream, the stream and y (less their means)
 #pragma unroll
@@ -323,7 +356,7 @@ __global__ __launch_bounds__(64 * block_waves(W)) void block_norm_backward_kerne
           mean[0] += o[i][e];
           mean[1] += y[i][e];
         }
-      row_sums<W>(mean, a.lanes, slot);
+      row_sums<W, P::kWaves>(mean, a.lanes, slot);
       const float mo = a.pre == OCCULT_NORM_LAYER ? mean[0] * a.inv_d : 0.0f;
       const float my = a.post == OCCULT_NORM_LAYER ? mean[1] * a.inv_d : 0.0f;
 #pragma unroll
@@ -352,7 +385,7 @@ __global__ __launch_bounds__(64 * block_waves(W)) void block_norm_backward_kerne
         if (LAYER) s[3] = fmaf(g[e], w[e], s[3]);
       }
     }
-    row_sums<W>(s, a.lanes, slot);
+    row_sums<W, P::kWaves>(s, a.lanes, slot);
     if (a.pre) {
       const float r = 1.0f / sqrtf(fmaf(s[0], a.inv_d, a.pre_eps));
       const float m2 = s[2] * r * a.inv_d, m1 = LAYER && a.pre == OCCULT_NORM_LAYER ? s[3] * a.inv_d : 0.0f;
@@ -413,7 +446,7 @@ __global__ __launch_bounds__(64 * block_waves(W)) void block_norm_backward_kerne
       }
       if (a.gate_kind == OCCULT_GATE_ELEMENT && a.dgate && valid && in) R::store_round(a.dgate, t, a.row_vecs, c, dg);
     }
-    if (a.post || a.gate_kind == OCCULT_GATE_TOKEN) row_sums<W>(u, a.lanes, slot);
+    if (a.post || a.gate_kind == OCCULT_GATE_TOKEN) row_sums<W, P::kWaves>(u, a.lanes, slot);
     if (a.gate_kind == OCCULT_GATE_TOKEN && a.dgate && valid && p.lane == 0) static_cast<float*>(a.dgate)[t] = u[2];
     const float m2 = a.post ? u[0] * a.inv_d : 0.0f, m1 = LAYER && a.post == OCCULT_NORM_LAYER ? u[1] * a.inv_d : 0.0f;
 #pragma unroll
@@ -427,8 +460,8 @@ __global__ __launch_bounds__(64 * block_waves(W)) void block_norm_backward_kerne
   }
 
   if (!a.sums) return;
-  constexpr int kThreads = Place<V, W>::kWaves * 64;
-  __shared__ float s_col[W < 4 ? kThreads * V * NE : 1];   // from four waves on a workgroup has one row at a time
+  constexpr int kThreads = P::kWaves * 64;
+  __shared__ float s_col[W < P::kWaves ? kThreads * V * NE : 1];   // unused where a workgroup has one row at a time
   const int d = a.row_vecs * NE;
   float* ws = a.ws + (size_t)blockIdx.x * __popc(a.sums) * d;
 #pragma unroll
@@ -492,26 +525,30 @@ __global__ __launch_bounds__(1024) void column_sums_kernel(const ColumnArgs a) {
   }
 }
 
-// Vectors per lane, waves per row and lanes per row of a row length: V and W of the kernels above.
+// Vectors per lane, waves per row and lanes per row of a row length: V and W of the kernels above.  Forward: two vectors per lane before a
+// second wave (16384 rows of 2048 bf16: 47 us, with one 51, with four 51; one row 3.3, 2.8, 4.6).  Backward: one vector per lane up to eight
+// waves (the column sums take registers: 1000 rows of 2048 12.8 us, with two 15.8; 16384 rows the same 76, with
+// means and biases 92 against 126), two beyond.
 struct Shape {
   int V, W, lanes;
 };
-static Shape shape_of(int row_vecs, int v_max) {
+static Shape shape_of(int row_vecs, bool backward) {
   Shape s{1, 1, 64};
   if (row_vecs <= 64) {
     while (s.lanes > 1 && s.lanes / 2 >= row_vecs) s.lanes /= 2;
     return s;
   }
-  while (s.V < v_max && 64 * s.V < row_vecs) s.V *= 2;
-  while (s.W < 16 && 64 * s.V * s.W < row_vecs) s.W *= 2;
+  if (!backward || row_vecs > 512) s.V = 2;
+  while (64 * s.V * s.W < row_vecs) s.W *= 2;   // rows up to kMaxRowBytes: 16 waves of 2
   return s;
 }
-static int rows_per_block(const Shape& s) { return s.W == 1 ? 4 * (64 / s.lanes) : (s.W < 4 ? 4 / s.W : 1); }
-
-constexpr int kForwardV = 4, kBackwardV = 2;
+static int rows_per_block(const Shape& s, bool backward) {
+  const int waves = block_waves(s.W, backward);
+  return s.W == 1 ? waves * (64 / s.lanes) : waves / s.W;
+}
 
 static int backward_blocks(const occult_cfg_t& c) {
-  const int rows = rows_per_block(shape_of(c.d * elem_size(c) / 16, kBackwardV));
+  const int rows = rows_per_block(shape_of(c.d * elem_size(c) / 16, true), true);
   const long long need = ((long long)c.T + rows - 1) / rows;
   return need < kBackwardBlocks ? (int)need : kBackwardBlocks;
 }
@@ -557,21 +594,21 @@ static int popcount(int v) { return __builtin_popcount((unsigned)v); }
 
 template <bool BF16>
 static int launch_forward(const Args& a, const Shape& s, hipStream_t stream) {
-  const int rows = rows_per_block(s);
+  const int rows = rows_per_block(s, false);
   const long long need = ((long long)a.T + rows - 1) / rows;
   const int grid = need < 4096 ? (int)need : 4096;
 #define OCC_NORM_CASE(V_, W_)                                                                             \
   if (s.V == V_ && s.W == W_) {                                                                           \
-    block_norm_kernel<BF16, V_, W_><<<grid, Place<V_, W_>::kWaves * 64, 0, stream>>>(a);                  \
+    block_norm_kernel<BF16, V_, W_><<<grid, 64 * block_waves(W_, false), 0, stream>>>(a);                 \
     OCC_LAUNCH_CHECK("block_norm_kernel");                                                                \
     return OCCULT_OK;                                                                                     \
   }
   OCC_NORM_CASE(1, 1)
   OCC_NORM_CASE(2, 1)
-  OCC_NORM_CASE(4, 1)
-  OCC_NORM_CASE(4, 2)
-  OCC_NORM_CASE(4, 4)
-  OCC_NORM_CASE(4, 8)
+  OCC_NORM_CASE(2, 2)
+  OCC_NORM_CASE(2, 4)
+  OCC_NORM_CASE(2, 8)
+  OCC_NORM_CASE(2, 16)
 #undef OCC_NORM_CASE
   OCC_FAIL(OCCULT_ESHAPE, "no kernel for rows of %d vectors", a.row_vecs);
 }
@@ -580,14 +617,14 @@ template <bool BF16, bool LAYER>
 static int launch_backward(const BackwardArgs& a, const Shape& s, int grid, hipStream_t stream) {
 #define OCC_NORM_CASE(V_, W_)                                                                             \
   if (s.V == V_ && s.W == W_) {                                                                           \
-    block_norm_backward_kernel<BF16, V_, W_, LAYER><<<grid, Place<V_, W_>::kWaves * 64, 0, stream>>>(a);  \
+    block_norm_backward_kernel<BF16, V_, W_, LAYER><<<grid, 64 * block_waves(W_, true), 0, stream>>>(a);  \
     OCC_LAUNCH_CHECK("block_norm_backward_kernel");                                                       \
     return OCCULT_OK;                                                                                     \
   }
   OCC_NORM_CASE(1, 1)
-  OCC_NORM_CASE(2, 1)
-  OCC_NORM_CASE(2, 2)
-  OCC_NORM_CASE(2, 4)
+  OCC_NORM_CASE(1, 2)
+  OCC_NORM_CASE(1, 4)
+  OCC_NORM_CASE(1, 8)
   OCC_NORM_CASE(2, 8)
   OCC_NORM_CASE(2, 16)
 #undef OCC_NORM_CASE
@@ -622,7 +659,7 @@ extern "C" int occult_block_norm(const occult_cfg_t* cfg, const occult_block_nor
   a.post = n->post_kind; a.pre = n->pre_kind; a.gate_kind = n->gate_kind;
   a.x_scale = n->x_scale; a.y_scale = n->y_scale; a.post_eps = n->post_eps; a.pre_eps = n->pre_eps;
   a.offset = n->weight_offset; a.inv_d = 1.0f / (float)c.d;
-  const Shape s = shape_of(a.row_vecs, kForwardV);
+  const Shape s = shape_of(a.row_vecs, false);
   a.lanes = s.lanes;
   hipStream_t st = static_cast<hipStream_t>(stream);
   return c.dtype == OCCULT_BF16 ? launch_forward<true>(a, s, st) : launch_forward<false>(a, s, st);
@@ -680,7 +717,7 @@ extern "C" int occult_block_norm_backward(const occult_cfg_t* cfg, const occult_
   a.offset = n->weight_offset; a.inv_d = 1.0f / (float)c.d;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (c.T > 0) {
-    const Shape s = shape_of(a.row_vecs, kBackwardV);
+    const Shape s = shape_of(a.row_vecs, true);
     a.lanes = s.lanes;
     const bool layer = n->post_kind == OCCULT_NORM_LAYER || n->pre_kind == OCCULT_NORM_LAYER || (sums & 10);
     if (c.dtype == OCCULT_BF16)

@@ -8,6 +8,8 @@ call is one call into the C library on the current stream, and nothing here sync
 """
 from __future__ import annotations
 
+import ctypes
+
 import torch
 
 from . import binding as B
@@ -19,11 +21,11 @@ _GATES = {None: B.OCCULT_GATE_NONE, "channel": B.OCCULT_GATE_CHANNEL, "token": B
 class BlockNorm:
     """post, pre: "rms", "layer" or None (no norm there); gate: "channel" ([d]), "token" ([T]), "element" ([T, d]) or None.
     Parameters are passed to the calls: weights and biases [d] and the gate in the layer's type, each may be left out
-    (factor 1, summand 0)."""
+    (factor 1, summand 0; a gate that the kind asks for has to be there)."""
 
     def __init__(self, T, d, dtype="bf16", post=None, pre="rms", gate=None, x_scale=1.0, y_scale=1.0, post_eps=1e-6, pre_eps=1e-6,
                  weight_offset=0.0, device="cuda:0"):
-        B.load_library()          # fail early and loudly if the HIP library is missing
+        self._lib = B.load_library()          # fail early and loudly if the HIP library is missing
         for name, kind, known in (("post", post, _NORMS), ("pre", pre, _NORMS), ("gate", gate, _GATES)):
             if kind not in known:
                 raise ValueError(f"occult: {name} is {kind!r}, known are {sorted(k for k in known if k)} and None")
@@ -37,38 +39,40 @@ class BlockNorm:
         self._fixed = (_NORMS[post], _NORMS[pre], _GATES[gate], x_scale, y_scale, post_eps, pre_eps, weight_offset)
         self._gate_len = {None: 0, "channel": d, "token": T, "element": T * d}[gate]
         B.occult_block_norm_backward_ws_bytes(self.cfg, B.make_block_norm(_NORMS[post], _NORMS[pre], 0, *self._fixed[3:]))  # checks both
+        self.desc = B.make_block_norm(*self._fixed)   # its parameters are set by every call
         self.out = torch.zeros((T, d), dtype=self.tdtype, device=self.device)
         self.h = torch.zeros((T, d), dtype=self.tdtype, device=self.device)
 
-    def _expect(self, t, name, numel):
-        if t is not None and t.device != self.device:
+    def _at(self, t, name, numel):
+        """Device address of a caller's tensor (None passes through), with binding's checks of it in one place: on small batches
+        the host's work is as long as the GPU's."""
+        if t is None:
+            return None
+        if t.get_device() != self.device.index:
             raise ValueError(f"occult: {name} is on {t.device}, the buffers are on {self.device}")
-        return B.expect(t, name, self.tdtype, numel)
+        B.expect(t, name, self.tdtype, numel)
+        return B._ptr(t)
 
-    def _rows(self, t, name):
-        return self._expect(t, name, self.T * self.d)
-
-    def _on_device(self):
-        """The library launches on the current device's stream."""
-        if torch.cuda.current_device() != self.device.index:
+    def _describe(self, gate, post_weight, post_bias, pre_weight, pre_bias):
+        if torch.cuda.current_device() != self.device.index:   # the library launches on the current device's stream
             raise ValueError(f"occult: the current device is cuda:{torch.cuda.current_device()}, the buffers are on {self.device}")
-
-    def _norm(self, gate, post_weight, post_bias, pre_weight, pre_bias):
-        self._on_device()
-        for t, name in ((post_weight, "post_weight"), (post_bias, "post_bias"), (pre_weight, "pre_weight"), (pre_bias, "pre_bias")):
-            self._expect(t, name, self.d)
-        self._expect(gate, "gate", self._gate_len)
-        return B.make_block_norm(*self._fixed, post_weight, post_bias, pre_weight, pre_bias, gate)
+        desc, d = self.desc, self.d
+        desc.post_weight = self._at(post_weight, "post_weight", d)
+        desc.post_bias = self._at(post_bias, "post_bias", d)
+        desc.pre_weight = self._at(pre_weight, "pre_weight", d)
+        desc.pre_bias = self._at(pre_bias, "pre_bias", d)
+        desc.gate = self._at(gate, "gate", self._gate_len)
+        return desc
 
     def forward(self, x, y=None, gate=None, post_weight=None, post_bias=None, pre_weight=None, pre_bias=None, out=None, h=None):
         """x, y [T, d] -> out [T, d], h [T, d] (None without a pre norm); without y the pre norm alone: out is x.
         Results go to this object's buffers unless others are given (out may be x, the residual stream in place)."""
-        norm = self._norm(gate, post_weight, post_bias, pre_weight, pre_bias)
+        desc = self._describe(gate, post_weight, post_bias, pre_weight, pre_bias)
+        n = self.T * self.d
         out = None if y is None else self.out if out is None else out
         h = None if self.pre is None else self.h if h is None else h
-        for t, name in ((x, "x"), (y, "y"), (out, "out"), (h, "h")):
-            self._rows(t, name)
-        B.occult_block_norm(self.cfg, norm, x, y, out, h)
+        B._check(self._lib.occult_block_norm(ctypes.byref(self.cfg), ctypes.byref(desc), self._at(x, "x", n), self._at(y, "y", n),
+                                             self._at(out, "out", n), self._at(h, "h", n), B._stream(None)))
         return (x if y is None else out), h
 
     def _buf(self, name, shape, dtype):
@@ -82,10 +86,10 @@ class BlockNorm:
         whether dy is wanted), dout the gradient of out from where it is read beside h (None = none), dh that
         of h -> dict of dx, dy, dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias: each None where there is
         nothing of that name; sums over tokens are f32 (accumulate: added to what the last call left)."""
-        norm = self._norm(gate, post_weight, post_bias, pre_weight, pre_bias)
-        for t, name in ((out, "out"), (dout, "dout"), (dh, "dh"), (y, "y")):
-            self._rows(t, name)
+        desc = self._describe(gate, post_weight, post_bias, pre_weight, pre_bias)
         T, d, f32 = self.T, self.d, torch.float32
+        n = T * d
+        rows = [self._at(t, name, n) for t, name in ((y, "y"), (out, "out"), (dout, "dout"), (dh, "dh"))]
         want_dy = y is not None if want_dy is None else want_dy
         g = {"dx": self._buf("dx", (T, d), self.tdtype), "dy": self._buf("dy", (T, d), self.tdtype) if want_dy else None}
         for name, given in (("dpost_weight", post_weight), ("dpost_bias", post_bias), ("dpre_weight", pre_weight),
@@ -96,10 +100,14 @@ class BlockNorm:
             shape, dtype = {"channel": ((d,), f32), "token": ((T,), f32), "element": ((T, d), self.tdtype)}[self.gate]
             g["dgate"] = self._buf("dgate", shape, dtype)
         ws = None
-        n = B.occult_block_norm_backward_ws_bytes(self.cfg, norm)
-        if n:
-            if getattr(self, "ws", None) is None or self.ws.numel() * 4 < n:
-                self.ws = torch.empty(n // 4, dtype=f32, device=self.device)
+        need = B.occult_block_norm_backward_ws_bytes(self.cfg, desc)
+        if need:
+            if getattr(self, "ws", None) is None or self.ws.numel() * 4 < need:
+                self.ws = torch.empty(need // 4, dtype=f32, device=self.device)
             ws = self.ws
-        B.occult_block_norm_backward(self.cfg, norm, y, out, dout, dh, accumulate=accumulate, ws=ws, **g)
+        at = {name: None if t is None else t.data_ptr() for name, t in g.items()}   # this object's own buffers
+        grads = B.occult_block_norm_grads_t(at["dpost_weight"], at["dpost_bias"], at["dpre_weight"], at["dpre_bias"], at["dgate"])
+        B._check(self._lib.occult_block_norm_backward(
+            ctypes.byref(self.cfg), ctypes.byref(desc), *rows, at["dx"], at["dy"], ctypes.byref(grads), int(bool(accumulate)),
+            None if ws is None else ws.data_ptr(), need, B._stream(None)))
         return g

@@ -3,8 +3,8 @@
 Bars.  A stored bf16 value is off by one rounding, BF16_U of its value (f32: 2^-24).  The float32 arithmetic before it: a row's sums
 add at most 8 * 4 values per lane, then 6 lane exchanges and 8 waves (46 additions), and a term passes fewer than 16 further
 operations, so every term of a result is off by less than 64 * 2^-24 = 2^-18 of its magnitude; a gradient of a norm multiplies
-three such sums, hence 2^-16; sums over tokens add at most 64 further steps here (T <= 2100 tokens over at least 33 row groups, 256
-groups of a workgroup, 32 + 16 workgroups: fewer than 400 additions), hence 2^-14.  The oracle returns the sum of the magnitudes of each result's terms,
+three such sums, hence 2^-16; sums over tokens add fewer than 600 times here (at most 9 rows per row group, 512
+groups of a workgroup, 16 + 16 workgroups), hence 2^-14.  The oracle returns the sum of the magnitudes of each result's terms,
 and the bars are relative to that."""
 import numpy as np
 import pytest
