@@ -201,6 +201,12 @@ def _stream(stream) -> Optional[int]:
     return stream.cuda_stream or None
 
 
+def _stream_of(device_index: int) -> Optional[int]:
+    """The current stream of a device as an address, without the Stream object around it (which takes as long as a launch)."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device_index) or None
+
+
 def make_cfg(T, d, f, E, S, k, D, dtype, n_d=0, prune_mode=1, renorm=1, expert_pos=None,
              sim_table=None) -> occult_cfg_t:
     """expert_pos: int32 device tensor [E] or None; sim_table: int32 device tensor [E, E-1] or None;
@@ -478,9 +484,10 @@ def occult_pack_w4(cfg, group, codes, scales, zeros, packed, stream=None) -> Non
 
 
 def occult_expert_ffn_w4(cfg, plan, sfd_x, x, packed, group, zeros, epd_h, epd_y, h_shared=None, y_shared=None, stream=None) -> None:
+    s = _stream_of(x.get_device()) if stream is None and x is not None and x.is_cuda else _stream(stream)
     _check(load_library().occult_expert_ffn_w4(ctypes.byref(cfg), ctypes.byref(plan), _ptr(sfd_x), _ptr(x), _ptr(packed),
                                                packed.numel() * packed.element_size(), int(group), int(bool(zeros)), _ptr(epd_h),
-                                               _ptr(epd_y), _ptr(h_shared), _ptr(y_shared), _stream(stream)))
+                                               _ptr(epd_y), _ptr(h_shared), _ptr(y_shared), s))
 
 
 def occult_forward_w4(cfg, plan, logits, x, packed, group, zeros, ids, w, plan_ws, sfd_x, epd_h, epd_y, h_shared, y_shared, sfd_y, y,

@@ -42,6 +42,8 @@ class BlockNorm:
         self.desc = B.make_block_norm(*self._fixed)   # its parameters are set by every call
         self.out = torch.zeros((T, d), dtype=self.tdtype, device=self.device)
         self.h = torch.zeros((T, d), dtype=self.tdtype, device=self.device)
+        self.ws = None
+        self.dx = self.dy = self.dgate = self.dpost_weight = self.dpost_bias = self.dpre_weight = self.dpre_bias = None
 
     def _at(self, t, name, numel):
         """Device address of a caller's tensor (None passes through), with binding's checks of it in one place: on small batches
@@ -72,13 +74,16 @@ class BlockNorm:
         out = None if y is None else self.out if out is None else out
         h = None if self.pre is None else self.h if h is None else h
         B._check(self._lib.occult_block_norm(ctypes.byref(self.cfg), ctypes.byref(desc), self._at(x, "x", n), self._at(y, "y", n),
-                                             self._at(out, "out", n), self._at(h, "h", n), B._stream(None)))
+                                             self._at(out, "out", n), self._at(h, "h", n),
+                                             B._stream_of(self.device.index)))
         return (x if y is None else out), h
 
     def _buf(self, name, shape, dtype):
-        if getattr(self, name, None) is None:
-            setattr(self, name, torch.zeros(shape, dtype=dtype, device=self.device))
-        return getattr(self, name)
+        t = getattr(self, name)
+        if t is None:
+            t = torch.zeros(shape, dtype=dtype, device=self.device)
+            setattr(self, name, t)
+        return t
 
     def backward(self, out, dout, dh=None, y=None, gate=None, post_weight=None, post_bias=None, pre_weight=None, pre_bias=None,
                  accumulate=False, want_dy=None):
@@ -91,23 +96,21 @@ class BlockNorm:
         n = T * d
         rows = [self._at(t, name, n) for t, name in ((y, "y"), (out, "out"), (dout, "dout"), (dh, "dh"))]
         want_dy = y is not None if want_dy is None else want_dy
-        g = {"dx": self._buf("dx", (T, d), self.tdtype), "dy": self._buf("dy", (T, d), self.tdtype) if want_dy else None}
-        for name, given in (("dpost_weight", post_weight), ("dpost_bias", post_bias), ("dpre_weight", pre_weight),
-                            ("dpre_bias", pre_bias)):
-            g[name] = None if given is None or (name.startswith("dpost") and not want_dy) else self._buf(name, (d,), f32)
-        g["dgate"] = None
+        g = {"dx": self._buf("dx", (T, d), self.tdtype), "dy": self._buf("dy", (T, d), self.tdtype) if want_dy else None,
+             "dpost_weight": self._buf("dpost_weight", (d,), f32) if post_weight is not None and want_dy else None,
+             "dpost_bias": self._buf("dpost_bias", (d,), f32) if post_bias is not None and want_dy else None,
+             "dpre_weight": self._buf("dpre_weight", (d,), f32) if pre_weight is not None else None,
+             "dpre_bias": self._buf("dpre_bias", (d,), f32) if pre_bias is not None else None, "dgate": None}
         if self.gate is not None and want_dy:
             shape, dtype = {"channel": ((d,), f32), "token": ((T,), f32), "element": ((T, d), self.tdtype)}[self.gate]
             g["dgate"] = self._buf("dgate", shape, dtype)
-        ws = None
-        need = B.occult_block_norm_backward_ws_bytes(self.cfg, desc)
-        if need:
-            if getattr(self, "ws", None) is None or self.ws.numel() * 4 < need:
-                self.ws = torch.empty(need // 4, dtype=f32, device=self.device)
-            ws = self.ws
+        if self.ws is None:   # enough for every parameter
+            full = B.make_block_norm(*self._fixed, *[self.h if k else None for k in (self.post, self.post, self.pre, self.pre, self.gate)])
+            self.ws = torch.empty(max(4, B.occult_block_norm_backward_ws_bytes(self.cfg, full) // 4), dtype=f32, device=self.device)
+            self._ws_bytes = self.ws.numel() * 4
         at = {name: None if t is None else t.data_ptr() for name, t in g.items()}   # this object's own buffers
         grads = B.occult_block_norm_grads_t(at["dpost_weight"], at["dpost_bias"], at["dpre_weight"], at["dpre_bias"], at["dgate"])
         B._check(self._lib.occult_block_norm_backward(
             ctypes.byref(self.cfg), ctypes.byref(desc), *rows, at["dx"], at["dy"], ctypes.byref(grads), int(bool(accumulate)),
-            None if ws is None else ws.data_ptr(), need, B._stream(None)))
+            self.ws.data_ptr(), self._ws_bytes, B._stream_of(self.device.index)))
         return g
