@@ -256,12 +256,12 @@ __device__ __forceinline__ Place find_place(const Args& first, const Args& secon
 
 // The four waves of a workgroup take the quarters of K of NB units of 16 output columns (NW matrices each: gate and up, or down) for up
 // to 16 rows of one group, and add their sums through LDS in the order of K.  For few rows, where the length of a wave's stream is
-// what counts: every wave has kRing - 1 K blocks in flight.
-template <int NB, int NW, int G, bool ZERO, bool F32>
+// what counts: every wave has kRing - 1 K blocks in flight (down product, whose waves have up to 11: 2 tokens, 64 experts and 2 shared
+// 9.1 us with three, 15.0 with one; gate/up, whose waves have four, 10.6 with one, in fewer registers, 12.7 with three).
+template <int NB, int NW, int G, bool ZERO, bool F32, int kRing>
 __device__ __forceinline__ void split_product(const Args& a, const TileInfo& ti, long long matrix, int unit0, float (*s_red)[NB * NW * 4][64]) {
   constexpr int kSteps = kBlockK / 32, kGroupSteps = kSteps / G;
   constexpr int P = XFrag<F32>::kParts;
-  constexpr int kRing = F32 ? 2 : 4;
   typedef Block<G, ZERO> B;
   const int units = (a.g.N + kUnit - 1) / kUnit;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -380,13 +380,13 @@ __device__ __forceinline__ void split_product(const Args& a, const TileInfo& ti,
   }
 }
 
-template <int NB, int NW, int G, bool ZERO, bool F32>
+template <int NB, int NW, int G, bool ZERO, bool F32, int kRing>
 __global__ __launch_bounds__(256, 2) void w4_gemm(const Args first, const Args second, const int b_blocks) {
   __shared__ Place s_place;
   __shared__ float s_red[4][NB * NW * 4][64];
   const Place place = find_place<16>(first, second, b_blocks, NB, 16, NB, &s_place);
   if (place.ti.group < 0) return;
-  split_product<NB, NW, G, ZERO, F32>((int)blockIdx.x < b_blocks ? second : first, place.ti, place.matrix, place.cb * NB, s_red);
+  split_product<NB, NW, G, ZERO, F32, kRing>((int)blockIdx.x < b_blocks ? second : first, place.ti, place.matrix, place.cb * NB, s_red);
 }
 
 // The same product for more rows: the four waves of a workgroup take NB units each over the whole K, and share x: a K block of it
@@ -584,7 +584,7 @@ __global__ __launch_bounds__(256, MT * NB > 2 ? 2 : MT == 2 && NW == 2 && (G == 
   if constexpr (SPLIT) {
     if (is_second) {
       static_assert(sizeof(float[4][NW * 4][64]) <= sizeof(s_x), "the sums fit where x would be");
-      split_product<1, NW, G, ZERO, false>(second, ti, place.matrix, place.cb, reinterpret_cast<float (*)[NW * 4][64]>(s_x));
+      split_product<1, NW, G, ZERO, false, 4>(second, ti, place.matrix, place.cb, reinterpret_cast<float (*)[NW * 4][64]>(s_x));
       return;
     }
   }
@@ -760,7 +760,7 @@ static int launch_typed(const Args& a, const Args* b, int group, bool zeros, int
 #define OCC_W4_CASE(G_, Z_)                                                                                                \
   if (group == kBlockK / G_ && zeros == Z_) {                                                                              \
     if constexpr (TILE) w4_tile_gemm<MT, NB, NW, G_, Z_, RING, SPLIT><<<(int)grid, 256, 0, s>>>(a, second, (int)b_blocks);        \
-    else w4_gemm<NB, NW, G_, Z_, F32><<<(int)grid, 256, 0, s>>>(a, second, (int)b_blocks);                                 \
+    else w4_gemm<NB, NW, G_, Z_, F32, RING><<<(int)grid, 256, 0, s>>>(a, second, (int)b_blocks);                                 \
     OCC_LAUNCH_CHECK(TILE ? "w4_tile_gemm" : "w4_gemm");                                                                   \
     return OCCULT_OK;                                                                                                      \
   }
@@ -780,19 +780,20 @@ template <int NW>
 static int launch(const occult_cfg_t& c, const Args& a, const Args* b, int group, bool zeros, hipStream_t s) {
   const int rows = c.T * c.k;
   if (c.dtype == OCCULT_F32) return launch_typed<false, 1, 2, NW, true, 2>(a, b, group, zeros, rows, s);
-  // K split over the waves while whole-K workgroups would not fill the chip one and a half times: 1 token, gate/up 9.1 against
-  // 12.2 us (60 experts), 2 tokens 12.6 against 14.7 (64: 256 workgroups); 4 tokens 16.1 against 14.3 (60: 440)
+  // K split over the waves while whole-K workgroups would not fill the chip two or three times: gate/up, 1 token 8.9 against
+  // 13.0 us (60 experts), 2 tokens 10.9 against 15.8 (64, none shared), 3 tokens 15.5 against 18.9 (64, 6 per token, 2 shared: 440
+  // workgroups); equal from 6 tokens on (60: 616).  Down: 2 tokens 10.0 against 15.0 (64, 2 shared: 416), 3 tokens 11.0 against 17.2 (608).
   const long long tiles = min_i(rows, rows / 16 + c.E) + (b ? (long long)b->g.ngroups * ((c.T + 15) / 16) : 0);
-  if (tiles * ((a.g.N + 4 * kUnit - 1) / (4 * kUnit)) <= 384) return launch_typed<false, 1, NW == 2 ? 1 : 2, NW, false, 2>(a, b, group, zeros, rows, s);
+  if (tiles * ((a.g.N + 4 * kUnit - 1) / (4 * kUnit)) <= 640)
+    return launch_typed<false, 1, 1, NW, false, NW == 2 ? 2 : 4>(a, b, group, zeros, rows, s);
   const long long per_expert = rows / c.E;
   if constexpr (NW == 1) {
-    // A long sum over the shared experts' matrices beside short routed ones (4 shared experts: 44 K blocks): 17 tokens split 20.1 against
-    // 25.8 us; 64 tokens split 33.0, codes three blocks ahead 27.8, one ahead 32.2; 128 tokens 33.9 against 38.1.  With 2 or none shared
-    // nothing is gained (64 experts, 17 tokens 18.8 against 16.6).
-    if (b && b->mats * b->kblocks >= 32) {
-      if (c.T <= 48) return launch_typed<true, 1, 1, 1, false, 4, true>(a, b, group, zeros, rows, s);
-      if (per_expert < 12) return launch_typed<true, 1, 1, 1, false, 4>(a, b, group, zeros, rows, s);
-    }
+    // A long sum over the shared experts' matrices beside short routed ones (K blocks: 44 of 4 shared experts, 22 of 2): 17 tokens split 20.1
+    // against 25.8 us; 64 tokens split 33.0, codes three blocks ahead 27.8, one ahead 32.2; 128 tokens 33.9 against 38.1.  With 2
+    // shared, 17 tokens 20.8 against 20.3; with none there is nothing to split, and codes further ahead only take registers.
+    const int chain = b ? b->mats * b->kblocks : 0;
+    if (chain >= 20 && chain >= c.T) return launch_typed<true, 1, 1, 1, false, 4, true>(a, b, group, zeros, rows, s);
+    if (chain >= 32 && per_expert < 12) return launch_typed<true, 1, 1, 1, false, 4>(a, b, group, zeros, rows, s);
   }
   // Tiles of 32 rows decode an expert's codes half as often as tiles of 16, and with two units per wave x is read half as often; both take
   // registers, and so waves that hide latency.  Gate/up, us, 16 rows | 32 rows | 32 rows and two units: 8 rows per expert 50.2 | 55.3 | 52.6;
