@@ -14,6 +14,8 @@
 #include "gemm.h"
 #include "stream_gemm.h"
 
+#include <type_traits>
+
 namespace occult {
 
 namespace w4 {
@@ -414,7 +416,11 @@ __device__ __forceinline__ void tile_product(const Args& a, const TileInfo& ti, 
 #pragma unroll
     for (int i = 0; i < MB; ++i) src[i] = a.g.a_rows[src[i]];
   }
-  const char* xrow[MB];   // set below, when the first codes have been asked for
+  const char* xrow[MB];
+  auto set_rows = [&]() {   // when the first codes have been asked for
+#pragma unroll
+    for (int i = 0; i < MB; ++i) xrow[i] = static_cast<const char*>(a.g.A) + (long long)src[i] * a.g.lda * 2 + piece * 16;
+  };
   const int blocks = a.kblocks * a.mats;
 
   struct Stage {
@@ -432,42 +438,48 @@ __device__ __forceinline__ void tile_product(const Args& a, const TileInfo& ti, 
   }
   const unsigned lane16 = lane * 16, scale_off = r * B::kScaleBytes;
   int code_kin = 0;
-  auto load_codes = [&](Stage& st) {   // the next K block's
+  // the K block that `code_at` stands at, one weight matrix of it; and on to the next K block
+  auto load_code = [&](B& w, int nb, int m) {
+    w.load(code_at[nb] + m * kBlockBytes, scale_at[nb] + m * (kUnit * B::kScaleBytes), lane16, scale_off);
+  };
+  auto advance_codes = [&]() {
+    const bool wraps = NW == 1 && ++code_kin == a.kblocks;   // on to the next matrix (gate and up have one)
+    if (wraps) code_kin = 0;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      // held in scalar registers: the compiler would carry base plus lane offset along per lane, a 64-bit addition for every load
-      asm volatile("" : "+s"(code_at[nb]), "+s"(scale_at[nb]));
-#pragma unroll
-      for (int m = 0; m < NW; ++m)
-        st.w[nb][m].load(code_at[nb] + m * kBlockBytes, scale_at[nb] + m * (kUnit * B::kScaleBytes), lane16, scale_off);
       code_at[nb] += NW * kBlockBytes;
       scale_at[nb] += NW * kUnit * B::kScaleBytes;
-    }
-    if (NW == 1 && ++code_kin == a.kblocks) {   // on to the next matrix (gate and up have one)
-      code_kin = 0;
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
+      if (wraps) {
         code_at[nb] += a.code_stride - (long long)a.kblocks * NW * kBlockBytes;
         scale_at[nb] += a.scale_stride - (long long)a.kblocks * NW * kUnit * B::kScaleBytes;
       }
+      // held in scalar registers: the compiler would carry base plus lane offset along per lane, a 64-bit addition for every load
+      asm volatile("" : "+s"(code_at[nb]), "+s"(scale_at[nb]));
     }
   };
+  auto load_codes = [&](B (&w)[NB][NW]) {   // the next K block's
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int m = 0; m < NW; ++m) load_code(w[nb][m], nb, m);
+    advance_codes();
+  };
   int x_kin = 0;
-  auto load_x = [&](Stage& st) {   // the next K block's
+  auto load_x = [&](u32x4 (&x)[MB]) {   // the next K block's
     const bool in = x_kin * kBlockK + piece * 8 < a.g.kseg;
     const bool wraps = ++x_kin == a.kblocks && NW == 1;
     const int step = wraps ? (a.g.kseg - (a.kblocks - 1) * kBlockK) * 2 : kBlockK * 2;
     if (wraps) x_kin = 0;
 #pragma unroll
     for (int i = 0; i < MB; ++i) {
-      st.x[i] = u32x4{0, 0, 0, 0};
-      if (in) st.x[i] = *reinterpret_cast<const u32x4*>(xrow[i]);
+      x[i] = u32x4{0, 0, 0, 0};
+      if (in) x[i] = *reinterpret_cast<const u32x4*>(xrow[i]);
       xrow[i] += step;
     }
   };
-  auto store_x = [&](const Stage& st, int buf) {
+  auto store_x = [&](const u32x4 (&x)[MB], int buf) {
 #pragma unroll
-    for (int i = 0; i < MB; ++i) *reinterpret_cast<u32x4*>(s_x + buf * kBuffer + (row_in + 16 * i) * kPitch + piece * 16) = st.x[i];
+    for (int i = 0; i < MB; ++i) *reinterpret_cast<u32x4*>(s_x + buf * kBuffer + (row_in + 16 * i) * kPitch + piece * 16) = x[i];
   };
 
   f32x4 acc[NB][NW][MB];
@@ -480,7 +492,8 @@ __device__ __forceinline__ void tile_product(const Args& a, const TileInfo& ti, 
 
   const bf16x8 minus24 = splat_bf16(0xC1C0u), ones = splat_bf16(0x3F80u);   // -(16 + 8); 1
   const unsigned sixteen = two_sixteens();
-  auto multiply = [&](const Stage& st, int buf) {
+  // refill: each matrix's registers are loaded again, with the next K block, as soon as its last group has been multiplied
+  auto multiply = [&](B (&w_all)[NB][NW], int buf, auto refill) {
 #pragma unroll
     for (int gi = 0; gi < G; ++gi) {
       bf16x8 xp[kGroupSteps][MB];
@@ -498,7 +511,7 @@ __device__ __forceinline__ void tile_product(const Args& a, const TileInfo& ti, 
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int m = 0; m < NW; ++m) {
-          const B& w = st.w[nb][m];
+          B& w = w_all[nb][m];
           const float scale = w.scale(gi);
           f32x4 part[MB];
 #pragma unroll
@@ -519,36 +532,55 @@ __device__ __forceinline__ void tile_product(const Args& a, const TileInfo& ti, 
           for (int tb = 0; tb < MB; ++tb)
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[nb][m][tb][e] = fmaf(scale, part[tb][e], acc[nb][m][tb][e]);
+          if constexpr (decltype(refill)::value) {
+            if (gi == G - 1) load_code(w, nb, m);
+          }
         }
       if constexpr (G > 1) __builtin_amdgcn_sched_barrier(0);   // or the next groups' x would be read early, and registers spilled
     }
   };
 
-  // codes and x kRing - 1 K blocks ahead in registers, x one ahead in LDS; one barrier per K block: whoever passes it has read the
-  // buffer that is written next
-  Stage ring[kRing];
-#pragma unroll
-  for (int i = 0; i < kRing - 1; ++i)
-    if (i < blocks) load_codes(ring[i]);   // before x, whose addresses wait for the row indices
-#pragma unroll
-  for (int i = 0; i < MB; ++i) xrow[i] = static_cast<const char*>(a.g.A) + (long long)src[i] * a.g.lda * 2 + piece * 16;
-#pragma unroll
-  for (int i = 0; i < kRing - 1; ++i)
-    if (i < blocks) load_x(ring[i]);
-  store_x(ring[0], 0);
-  __syncthreads();
-  for (int kb = 0; kb < blocks;) {   // uniform over the workgroup
-#pragma unroll
-    for (int i = 0; i < kRing; ++i) {
-      Stage& next = ring[(i + kRing - 1) % kRing];
-      if (kb + kRing - 1 < blocks) {
-        load_x(next);
-        load_codes(next);
-      }
-      multiply(ring[i], i & 1);
-      if (++kb == blocks) break;
-      store_x(ring[(i + 1) % kRing], 1 - (i & 1));
+  // x one K block ahead in LDS; one barrier per K block: whoever passes it has read the buffer that is written next
+  if constexpr (kRing == 1) {   // codes one K block ahead in the registers of the block before
+    B w[NB][NW];
+    u32x4 x[MB];
+    load_codes(w);   // before x, whose addresses wait for the row indices
+    set_rows();
+    load_x(x);
+    store_x(x, 0);
+    __syncthreads();
+    for (int kb = 0; kb + 1 < blocks; ++kb) {   // uniform over the workgroup
+      load_x(x);
+      multiply(w, kb & 1, std::true_type{});
+      advance_codes();
+      store_x(x, 1 - (kb & 1));
       __syncthreads();
+    }
+    multiply(w, (blocks - 1) & 1, std::false_type{});
+  } else {                      // codes and x kRing - 1 K blocks ahead in registers
+    Stage ring[kRing];
+#pragma unroll
+    for (int i = 0; i < kRing - 1; ++i)
+      if (i < blocks) load_codes(ring[i].w);
+    set_rows();
+#pragma unroll
+    for (int i = 0; i < kRing - 1; ++i)
+      if (i < blocks) load_x(ring[i].x);
+    store_x(ring[0].x, 0);
+    __syncthreads();
+    for (int kb = 0; kb < blocks;) {   // uniform over the workgroup
+#pragma unroll
+      for (int i = 0; i < kRing; ++i) {
+        Stage& next = ring[(i + kRing - 1) % kRing];
+        if (kb + kRing - 1 < blocks) {
+          load_x(next.x);
+          load_codes(next.w);
+        }
+        multiply(ring[i].w, i & 1, std::false_type{});
+        if (++kb == blocks) break;
+        store_x(ring[(i + 1) % kRing].x, 1 - (i & 1));
+        __syncthreads();
+      }
     }
   }
 
@@ -572,9 +604,9 @@ __device__ __forceinline__ void tile_product(const Args& a, const TileInfo& ti, 
 // projection walks the matrices of all of them: with 4 of them and the whole K to a wave, 44 K blocks one after the other, which took
 // longer than the routed experts' whole product up to 64 tokens (17 tokens, 4 of 60 experts: 26.3 us, split 19.0).
 template <int MT, int NB, int NW, int G, bool ZERO, int kRing, bool SPLIT>
-__global__ __launch_bounds__(256, MT * NB > 2 ? 2 : MT == 2 && NW == 2 && (G == 4 || !ZERO) ? 3 : MT == 1 && !SPLIT && !(G == 4 && ZERO) ? 5 : 4) void w4_tile_gemm(const Args first, const Args second, const int b_blocks) {
+__global__ __launch_bounds__(256, kRing == 1 ? 2 : 4) void w4_tile_gemm(const Args first, const Args second, const int b_blocks) {
   constexpr int BM = 16 * MT;
-  static_assert(kRing % 2 == 0, "the LDS buffers alternate");
+  static_assert(kRing == 1 || kRing % 2 == 0, "the LDS buffers alternate");
   __shared__ Place s_place;
   __shared__ __attribute__((aligned(16))) char s_x[2 * BM * kPitch];
   const Place place = find_place<BM>(first, second, b_blocks, 4 * NB, SPLIT ? 16 : BM, SPLIT ? 1 : 4 * NB, &s_place);
@@ -796,12 +828,13 @@ static int launch(const occult_cfg_t& c, const Args& a, const Args* b, int group
     if (chain >= 32 && per_expert < 12) return launch_typed<true, 1, 1, 1, false, 4>(a, b, group, zeros, rows, s);
   }
   // Tiles of 32 rows decode an expert's codes half as often as tiles of 16, and with two units per wave x is read half as often; both take
-  // registers, and so waves that hide latency.  Gate/up, us, 16 rows | 32 rows | 32 rows and two units: 8 rows per expert 50.2 | 55.3 | 52.6;
-  // 16 rows 69.4 | 67.4 | 72.2; 23 rows 72.4 | 66.9 | 64.6; 46 rows 116 | 106 | 98; with groups of 32 (four scalings per block)
-  // 23 rows 78.4 | 72.8 | 83.3, 46 rows 131 | 117 | 133.  Down product: 46 rows 81 | 74 | 60.
-  if (per_expert >= 20 && (NW == 1 || group != 32)) return launch_typed<true, 2, 2, NW, false, 2>(a, b, group, zeros, rows, s);
-  if (per_expert >= 16) return launch_typed<true, 2, 1, NW, false, 2>(a, b, group, zeros, rows, s);
-  return launch_typed<true, 1, 1, NW, false, 2>(a, b, group, zeros, rows, s);
+  // registers, and so waves that hide latency.  Gate/up, us, 16 rows | 32 rows | 32 rows and two units: 4 rows per expert 38.4 | 41.5 |
+  // 39.2; 8 rows 47.6 | 45.7 | 52.6; 16 rows 65.7 | 59.8 | 56.7; 23 rows 65.0 | 59.7 | 57.7; 46 rows 108 | 92 | 83; with groups
+  // of 32, whose four scalings per block take registers, 23 rows 72.3 | 67.0 | 71.0, 46 rows 137 | 119 | 125.  Down product: 12 rows
+  // 34.1 | 32.3 | 32.5; 16 rows 41.5 | 42.6 | 50.6; 23 rows 43.8 | 41.4 | 37.9; 46 rows 72 | 64 | 52.
+  if (per_expert >= (NW == 2 ? 16 : 20) && (NW == 1 || group != 32)) return launch_typed<true, 2, 2, NW, false, 1>(a, b, group, zeros, rows, s);
+  if (per_expert >= 8) return launch_typed<true, 2, 1, NW, false, 1>(a, b, group, zeros, rows, s);
+  return launch_typed<true, 1, 1, NW, false, 1>(a, b, group, zeros, rows, s);
 }
 
 }  // namespace w4
