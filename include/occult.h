@@ -271,14 +271,15 @@ int occult_expert_ffn_packed(const occult_cfg_t* cfg, const occult_plan_t* plan,
  *   zeros[] given of (max(w, 0) - min(w, 0)) / 15; zero = round(-min / scale); code = round(w / scale) + zero, clamped.
  *   A group of zeros gets scale 0 and codes 8.
  * occult_dequantize_weights writes the values they stand for in cfg.dtype, in the layout of occult_weights_t (rounded to nearest): for
- *   batches of hundreds of rows per expert, where occult_expert_ffn on them is the faster way.
+ *   batches of more than about 130 rows per expert, where occult_expert_ffn on them is the faster way.
  * occult_pack_w4 writes codes and scales in the order the products read them (occult_pack_w4_bytes() bytes, 16-byte aligned; nothing
  *   else is read afterwards): per matrix (gate and up in pairs) units of 16 rows, per unit K blocks of 128, per block and
  *   matrix 64 pieces of 16 bytes, piece l = row l % 16, whose dword j holds K elements j * 32 + (l / 16) * 8 .. + 8: element 2i in bits
  *   4i .. 4i + 3, 2i + 1 in bits 16 + 4i .., rotated left by 3.  Scales follow the codes of all matrices in the same order.
  * occult_expert_ffn_w4 is occult_expert_ffn computed from them: same plan, same rows, same outputs; products of x and codes are
  *   summed in f32 per group and scaled in f32 (f32 layers: x is not rounded either); h is rounded to cfg.dtype between the
- *   two products.  cfg.ffn_phase as there.  Row sums do not depend on T within a rule on T * k / E that picks the tile.
+ *   two products.  cfg.ffn_phase as there.  Which kernel computes a product, and with it the last bits, depends on T, E, k, S, d and
+ *   f; for one layer description results are the same bits every time.  A launch of 2^24 workgroups or more is refused (OCCULT_ESHAPE).
  * occult_forward_w4 is occult_forward with occult_expert_ffn_w4 in the place of the expert computation (no pre-activations
  *   are kept: buffers->epd_gu, gu_shared and ffn_ws are not used). */
 typedef struct occult_w4_weights {

@@ -600,23 +600,25 @@ __device__ __forceinline__ void tile_product(const Args& a, const TileInfo& ti, 
   }
 }
 
-// SPLIT: the second problem's workgroups take 16 rows of one unit with K split over the waves, as in w4_gemm.  The shared experts' down
-// projection walks the matrices of all of them: with 4 of them and the whole K to a wave, 44 K blocks one after the other, which took
-// longer than the routed experts' whole product up to 64 tokens (17 tokens, 4 of 60 experts: 26.3 us, split 19.0).
-template <int MT, int NB, int NW, int G, bool ZERO, int kRing, bool SPLIT>
+// SPLIT: the second problem's workgroups take 16 rows of SPLIT units with K split over the waves, as in w4_gemm (0: they are like the
+// first's).  The shared experts' down projection walks the matrices of all of them: with 4 of them and the whole K to a wave,
+// 44 K blocks one after the other, which takes longer than the routed experts' whole product up to 64 tokens.
+template <int MT, int NB, int NW, int G, bool ZERO, int kRing, int SPLIT>
 __global__ __launch_bounds__(256, kRing == 1 ? 2 : 4) void w4_tile_gemm(const Args first, const Args second, const int b_blocks) {
   constexpr int BM = 16 * MT;
   static_assert(kRing == 1 || kRing % 2 == 0, "the LDS buffers alternate");
   __shared__ Place s_place;
-  __shared__ __attribute__((aligned(16))) char s_x[2 * BM * kPitch];
-  const Place place = find_place<BM>(first, second, b_blocks, 4 * NB, SPLIT ? 16 : BM, SPLIT ? 1 : 4 * NB, &s_place);
+  constexpr int kLds = 2 * BM * kPitch > SPLIT * NW * 4096 ? 2 * BM * kPitch : SPLIT * NW * 4096;
+  __shared__ __attribute__((aligned(16))) char s_x[kLds];
+  const Place place = find_place<BM>(first, second, b_blocks, 4 * NB, SPLIT ? 16 : BM, SPLIT ? SPLIT : 4 * NB, &s_place);
   const TileInfo& ti = place.ti;
   if (ti.group < 0) return;
   const bool is_second = (int)blockIdx.x < b_blocks;   // uniform
   if constexpr (SPLIT) {
     if (is_second) {
-      static_assert(sizeof(float[4][NW * 4][64]) <= sizeof(s_x), "the sums fit where x would be");
-      split_product<1, NW, G, ZERO, false, 4>(second, ti, place.matrix, place.cb, reinterpret_cast<float (*)[NW * 4][64]>(s_x));
+      static_assert(sizeof(float[4][SPLIT * NW * 4][64]) <= sizeof(s_x), "the sums fit where x would be");
+      split_product<SPLIT, NW, G, ZERO, false, 3>(second, ti, place.matrix, place.cb * SPLIT,
+                                                  reinterpret_cast<float (*)[SPLIT * NW * 4][64]>(s_x));
       return;
     }
   }
@@ -629,11 +631,6 @@ __global__ __launch_bounds__(256, kRing == 1 ? 2 : 4) void w4_tile_gemm(const Ar
 }
 
 // ---- quantisation, values, packing ----------------------------------------------------------------------------------------
-template <bool BF16>
-__device__ __forceinline__ float load_weight(const void* p, size_t i) {
-  if constexpr (BF16) return __uint_as_float((unsigned)static_cast<const uint16_t*>(p)[i] << 16);
-  else return static_cast<const float*>(p)[i];
-}
 // double -> bf16, to nearest even, in one rounding
 __device__ __forceinline__ uint16_t bf16_of(double v) {
   float f = (float)v;
@@ -647,40 +644,63 @@ __device__ __forceinline__ uint16_t bf16_of(double v) {
 }
 __device__ __forceinline__ float bf16_value(uint16_t b) { return __uint_as_float((unsigned)b << 16); }
 
-// One thread per group.  Codes by division in double: the quotient of two floats is never so close to a rounding border that double
-// would put it on the other side.
+// group / 8 neighbouring lanes per group, 8 weights each.  Codes by division in double: the quotient of two floats is never so close to a
+// rounding border that double would put it on the other side.  (One thread per group of 128 read a line for every two bytes: 1.1 GB
+// of weights 20.7 ms, so 0.7.)
 template <bool BF16>
 __global__ __launch_bounds__(256) void quantize_kernel(const void* w, long long rows, int K, int group, uint8_t* codes, uint16_t* scales,
                                                        uint8_t* zeros) {
-  const int groups = (K + group - 1) / group;
-  const long long n = rows * groups;
+  const int groups = (K + group - 1) / group, lanes = group / 8;
+  const long long n = rows * groups * lanes;   // a multiple of `lanes`, like the stride: a group's lanes stay together
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
-    const long long row = i / groups;
-    const int k0 = (int)(i - row * groups) * group, k1 = min(K, k0 + group);
-    const size_t base = (size_t)row * K;
-    float lo = 0.0f, hi = 0.0f;
-    for (int k = k0; k < k1; ++k) {
-      const float v = load_weight<BF16>(w, base + k);
-      lo = fminf(lo, v);
-      hi = fmaxf(hi, v);
-    }
-    const double span = zeros ? ((double)hi - (double)lo) / 15.0 : (double)fmaxf(hi, -lo) / 7.0;
-    const uint16_t sb = bf16_of(span);
-    const double s = (double)bf16_value(sb);
-    int z = 8;
-    if (zeros) {
-      z = s > 0.0 ? (int)fmin(fmax(rint(-(double)lo / s), 0.0), 15.0) : 8;
-      zeros[i] = (uint8_t)z;
-    }
-    scales[i] = sb;
-    for (int k = k0; k < k1; k += 2) {
-      int q[2];
-      for (int e = 0; e < 2; ++e) {
-        const double t = s > 0.0 ? rint((double)load_weight<BF16>(w, base + k + e) / s) + z : (double)z;
-        q[e] = (int)fmin(fmax(t, 0.0), 15.0);
+    const long long at = i / lanes, row = at / groups;
+    const int k0 = (int)(at - row * groups) * group + (int)(i % lanes) * 8;
+    const size_t base = (size_t)row * K + k0;
+    float v[8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {   // K is a multiple of 4
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * h + e] = 0.0f;
+      if (k0 + 4 * h < K) {
+        if constexpr (BF16) {
+          const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(w) + base + 4 * h);
+          v[4 * h] = bf16_lo(u.x); v[4 * h + 1] = bf16_hi(u.x);
+          v[4 * h + 2] = bf16_lo(u.y); v[4 * h + 3] = bf16_hi(u.y);
+        } else {
+          const f32x4 u = *reinterpret_cast<const f32x4*>(static_cast<const float*>(w) + base + 4 * h);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[4 * h + e] = u[e];
+        }
       }
-      codes[(base + k) / 2] = (uint8_t)(q[0] | q[1] << 4);
     }
+    float lo = 0.0f, hi = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      lo = fminf(lo, v[e]);
+      hi = fmaxf(hi, v[e]);
+    }
+    for (int o = 1; o < lanes; o <<= 1) {
+      lo = fminf(lo, __shfl_xor(lo, o, 64));
+      hi = fmaxf(hi, __shfl_xor(hi, o, 64));
+    }
+    const uint16_t sb = bf16_of(zeros ? ((double)hi - (double)lo) / 15.0 : (double)fmaxf(hi, -lo) / 7.0);
+    const double s = (double)bf16_value(sb);
+    const int z = zeros && s > 0.0 ? (int)fmin(fmax(rint(-(double)lo / s), 0.0), 15.0) : 8;
+    if (i % lanes == 0) {
+      scales[at] = sb;
+      if (zeros) zeros[at] = (uint8_t)z;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (k0 + 4 * h < K) {
+        unsigned q = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const double t = s > 0.0 ? rint((double)v[4 * h + e] / s) + z : (double)z;
+          q |= (unsigned)fmin(fmax(t, 0.0), 15.0) << (4 * e);
+        }
+        reinterpret_cast<uint16_t*>(codes)[(base + 4 * h) / 4] = (uint16_t)q;
+      }
   }
 }
 
@@ -695,7 +715,7 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const uint8_t* codes, c
     const int k = (int)(i - row * quads) * 4;
     const long long g = row * groups + k / group;
     const float s = bf16_value(scales[g]);
-    const float z = zeros ? (float)zeros[g] : 8.0f;
+    const float z = zeros ? (float)(zeros[g] & 15) : 8.0f;
     const unsigned q = reinterpret_cast<const uint16_t*>(codes)[((size_t)row * K + k) / 4];
     float v[4];
 #pragma unroll
@@ -776,9 +796,9 @@ static int grid_for(long long threads) {
 }
 
 // TILE: w4_tile_gemm, whose workgroups have 4 * NB units (SPLIT: of the second problem one); else w4_gemm with NB
-template <bool TILE, int MT, int NB, int NW, bool F32, int RING, bool SPLIT = false>
+template <bool TILE, int MT, int NB, int NW, bool F32, int RING, int SPLIT = 0>
 static int launch_typed(const Args& a, const Args* b, int group, bool zeros, int total_rows, hipStream_t s) {
-  constexpr int BM = 16 * MT, UNITS = TILE ? 4 * NB : NB, B_ROWS = SPLIT ? 16 : BM, B_UNITS = SPLIT ? 1 : UNITS;
+  constexpr int BM = 16 * MT, UNITS = TILE ? 4 * NB : NB, B_ROWS = SPLIT ? 16 : BM, B_UNITS = SPLIT ? SPLIT : UNITS;
   const int n_cb = ((a.g.N + kUnit - 1) / kUnit + UNITS - 1) / UNITS;
   // row tiles of the grouped rows: at most one partly filled one per group, and none without a row
   long long m_tiles = ((long long)total_rows + (long long)a.g.ngroups * (BM - 1)) / BM;
@@ -820,11 +840,11 @@ static int launch(const occult_cfg_t& c, const Args& a, const Args* b, int group
     return launch_typed<false, 1, 1, NW, false, NW == 2 ? 2 : 4>(a, b, group, zeros, rows, s);
   const long long per_expert = rows / c.E;
   if constexpr (NW == 1) {
-    // A long sum over the shared experts' matrices beside short routed ones (K blocks: 44 of 4 shared experts, 22 of 2): 17 tokens split 20.1
-    // against 25.8 us; 64 tokens split 33.0, codes three blocks ahead 27.8, one ahead 32.2; 128 tokens 33.9 against 38.1.  With 2
-    // shared, 17 tokens 20.8 against 20.3; with none there is nothing to split, and codes further ahead only take registers.
+    // A long sum over the shared experts' matrices beside short routed ones (K blocks: 44 of 4 shared experts, 22 of 2): 4 tokens split 12.2
+    // against 24.3 us, 17 tokens 20.8 against 33.1, 64 tokens 27.7 against 38.4 (29.1 with codes three blocks ahead), 128 tokens 38.9
+    // against 40.7 (36.2 with codes three blocks ahead).  With 2 shared, 4 tokens 11.1 against 13.7, 17 tokens 22.8 against 22.7.
     const int chain = b ? b->mats * b->kblocks : 0;
-    if (chain >= 20 && chain >= c.T) return launch_typed<true, 1, 1, 1, false, 4, true>(a, b, group, zeros, rows, s);
+    if ((chain >= 20 && chain >= c.T) || (chain >= 32 && c.T <= 64)) return launch_typed<true, 1, 1, 1, false, 1, 2>(a, b, group, zeros, rows, s);
     if (chain >= 32 && per_expert < 12) return launch_typed<true, 1, 1, 1, false, 4>(a, b, group, zeros, rows, s);
   }
   // Tiles of 32 rows decode an expert's codes half as often as tiles of 16, and with two units per wave x is read half as often; both take
@@ -858,7 +878,7 @@ extern "C" int occult_quantize_weights(const occult_cfg_t* cfg, const occult_wei
   for (int i = 0; i < 3; ++i) {
     const int N = i < 2 ? c.f : c.d, K = i < 2 ? c.d : c.f;
     const long long rows = (long long)(c.E + c.S) * N;
-    const int grid = grid_for(rows * ((K + out->group - 1) / out->group));
+    const int grid = grid_for(rows * ((K + out->group - 1) / out->group) * (out->group / 8));
     if (c.dtype == OCCULT_BF16)
       quantize_kernel<true><<<grid, 256, 0, s>>>(w[i], rows, K, out->group, out->codes[i], out->scales[i], out->zeros[i]);
     else

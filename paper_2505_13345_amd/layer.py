@@ -189,23 +189,30 @@ class OccultLayer:
 
     def pack_weights_w4(self, w4):
         """4-bit weights in the order that expert_ffn_w4() and forward_w4() read (again after every change of the weights, which
-        are not read after this)."""
+        are not read after this).  Weights of the same group and kind of zero points go to the same buffer, also under a captured
+        graph; another group or kind takes a new buffer, which only graphs captured afterwards read."""
         self._expect_w4(w4)
-        n = B.occult_pack_w4_bytes(self.cfg, w4.group, w4.has_zeros)
-        if getattr(self, "packed_w4", None) is None or self.packed_w4.numel() < n:
-            self.packed_w4 = torch.empty(n, dtype=torch.uint8, device=self.device)
-        self.w4_format = (w4.group, w4.has_zeros)
-        B.occult_pack_w4(self.cfg, *w4, self.packed_w4)
-        return self.packed_w4
+        form = (w4.group, w4.has_zeros)
+        packed = getattr(self, "packed_w4", None)
+        if packed is None or self.w4_format != form:
+            packed = torch.empty(B.occult_pack_w4_bytes(self.cfg, *form), dtype=torch.uint8, device=self.device)
+        B.occult_pack_w4(self.cfg, *w4, packed)
+        self.packed_w4, self.w4_format = packed, form
+        return packed
 
     def _packed_w4(self):
         if getattr(self, "packed_w4", None) is None:
             raise ValueError("occult: no 4-bit weights: call pack_weights_w4() first")
         return (self.packed_w4, *self.w4_format)
 
+    def _here(self, x):
+        if x.is_cuda and x.get_device() != torch.cuda.current_device():   # the library launches on the current device's stream
+            raise ValueError(f"occult: the current device is cuda:{torch.cuda.current_device()}, x is on {x.device}")
+
     def expert_ffn_w4(self, x):
         """expert_ffn() from 4-bit weights -> epd_y, y_shared (None without shared experts)."""
         self._hidden(x, "x")
+        self._here(x)
         self.gu_saved = False
         B.occult_expert_ffn_w4(self.cfg, self.plan, self.sfd_x, x, *self._packed_w4(), self.epd_h, self.epd_y, self.h_shared,
                                self.y_shared)
@@ -223,6 +230,7 @@ class OccultLayer:
         s = self.shape
         B.expect(logits, "logits", torch.float32, s["T"] * s["E"])
         self._hidden(x, "x")
+        self._here(x)
         self.gu_saved = False
         B.occult_forward_w4(self.cfg, self.plan, logits, x, *self._packed_w4(), self.ids, self.w, self.ws, self.sfd_x, self.epd_h,
                             self.epd_y, self.h_shared, self.y_shared, self.sfd_y, self.y)

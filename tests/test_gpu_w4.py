@@ -128,6 +128,27 @@ def test_network_f32(shape, group, zeros):
     check_network(layer, x, values, tops, "f32", f"f32 {shape} {group} {zeros}")
 
 
+# enough workgroups for the kernels whose waves take the whole K (the layers above are computed with K split over the waves): 16-row tiles
+# in the first and in the second product; shared experts' long sums split, and with codes three blocks ahead; 32-row tiles, with
+# one and with two units per wave; odd widths, experts without rows, tiles with one and two blocks of rows
+TILED = [(20, 200, 648, 64, 4, 4, 4), (20, 648, 200, 64, 4, 4, 4), (18, 648, 640, 64, 4, 4, 4), (50, 648, 1032, 64, 4, 2, 4),
+         (70, 648, 1032, 64, 4, 3, 4), (60, 72, 1416, 16, 1, 4, 4), (60, 1416, 72, 16, 0, 4, 4), (60, 136, 2008, 8, 1, 4, 2),
+         (60, 2008, 136, 8, 0, 4, 2), (130, 264, 1928, 4, 2, 2, 2), (130, 1928, 264, 4, 2, 2, 2)]
+
+
+@pytest.mark.parametrize("shape", TILED)
+@pytest.mark.parametrize("group,zeros", [(32, False), (32, True), (64, False), (64, True), (128, False), (128, True)])
+def test_network_in_tiles(shape, group, zeros):
+    say(f"tiles {shape} group {group} zeros {zeros}")
+    layer, xd, _, _, values, tops, x = make(*shape, "bf16", group, zeros, seed=sum(shape))
+    layer.expert_ffn_w4(xd)
+    check_network(layer, x, values, tops, "bf16", f"{shape} {group} {zeros}")
+    first = [t.clone() for t in (layer.epd_y, layer.epd_h) + ((layer.y_shared, layer.h_shared) if shape[4] else ())]
+    layer.expert_ffn_w4(xd)
+    for a, b in zip(first, (layer.epd_y, layer.epd_h) + ((layer.y_shared, layer.h_shared) if shape[4] else ())):
+        assert torch.equal(a, b)   # sums in a fixed order
+
+
 def test_placed_experts_and_a_large_batch():
     layer, xd, _, _, values, tops, x = make(2500, 136, 72, 8, 1, 3, 4, "bf16", 64, True, seed=3, placement=5)
     layer.expert_ffn_w4(xd)
@@ -240,6 +261,46 @@ def test_refusals_of_the_buffers():
         layer.quantize_weights(*layer.dequantize_weights(q), group=20)
     with pytest.raises(ValueError, match="not in GPU memory"):
         layer.expert_ffn_w4(xd.cpu())
+
+
+def test_refusal_of_another_current_device(monkeypatch):
+    layer, xd, logits, *_ = make(5, 64, 96, 4, 0, 2, 2, "bf16", 32, True)
+    norm = BlockNorm(5, 64)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for call in (lambda: layer.expert_ffn_w4(xd), lambda: layer.forward_w4(logits, xd), lambda: norm.forward(xd),
+                 lambda: norm.backward(xd, None, xd)):
+        with pytest.raises(ValueError, match="current device"):
+            call()
+
+
+def test_weights_packed_again():
+    """The same format goes to the same buffer, which a captured graph goes on reading; another format takes a new one."""
+    layer, xd, _, q, *_ = make(9, 136, 72, 4, 1, 2, 2, "bf16", 32, True, seed=11)
+    other = make(9, 136, 72, 4, 1, 2, 2, "bf16", 32, True, seed=12)[3]
+    first = layer.expert_ffn_w4(xd)[0].clone()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        layer.expert_ffn_w4(xd)
+    torch.cuda.synchronize()
+    at = layer.packed_w4.data_ptr()
+    layer.pack_weights_w4(other)
+    assert layer.packed_w4.data_ptr() == at
+    second = layer.expert_ffn_w4(xd)[0].clone()
+    assert not torch.equal(first, second)
+    for weights, want in ((q, first), (other, second), (q, first)):
+        layer.pack_weights_w4(weights)
+        layer.epd_y.fill_(3.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(layer.epd_y, want)
+    keep = layer.packed_w4
+    layer.pack_weights_w4(layer.quantize_weights(*layer.dequantize_weights(q), group=64))
+    assert layer.packed_w4.data_ptr() != keep.data_ptr()
+    with pytest.raises(B.OccultError):
+        layer.pack_weights_w4(q._replace(group=16))
+    assert layer.w4_format == (64, False)
 
 
 def test_no_tokens():
