@@ -256,11 +256,10 @@ __device__ __forceinline__ Place find_place(const Args& first, const Args& secon
   return p;
 }
 
-// The four waves of a workgroup take the quarters of K of NB units of 16 output columns (NW matrices each: gate and up, or down) for up
+// The waves of a workgroup take equal parts of K of NB units of 16 output columns (NW matrices each: gate and up, or down) for up
 // to 16 rows of one group, and add their sums through LDS in the order of K.  For few rows, where the length of a wave's stream is
-// what counts: every wave has kRing - 1 K blocks in flight (down product, whose waves have up to 11: 2 tokens, 64 experts and 2 shared
-// 9.1 us with three, 15.0 with one; gate/up, whose waves have four, 10.6 with one, in fewer registers, 12.7 with three).
-template <int NB, int NW, int G, bool ZERO, bool F32, int kRing>
+// what counts; every wave has kRing - 1 K blocks in flight.
+template <int NB, int NW, int G, bool ZERO, bool F32, int kRing, int WAVES>
 __device__ __forceinline__ void split_product(const Args& a, const TileInfo& ti, long long matrix, int unit0, float (*s_red)[NB * NW * 4][64]) {
   constexpr int kSteps = kBlockK / 32, kGroupSteps = kSteps / G;
   constexpr int P = XFrag<F32>::kParts;
@@ -270,7 +269,7 @@ __device__ __forceinline__ void split_product(const Args& a, const TileInfo& ti,
   const int r = lane & 15, c = lane >> 4;
   // this wave's K blocks, counted through the matrices that K walks
   const int blocks = a.kblocks * a.mats;
-  const int kb_begin = blocks * wave / 4, kb_end = blocks * (wave + 1) / 4;
+  const int kb_begin = blocks * wave / WAVES, kb_end = blocks * (wave + 1) / WAVES;
 
   const char* xrow;
   {
@@ -356,7 +355,7 @@ __device__ __forceinline__ void split_product(const Args& a, const TileInfo& ti,
     }
   }
 
-  // the four waves' sums, added in the order of K; wave e finishes element e of every accumulator
+  // the waves' sums, added in the order of K; wave e < 4 finishes element e of every accumulator
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -364,13 +363,16 @@ __device__ __forceinline__ void split_product(const Args& a, const TileInfo& ti,
 #pragma unroll
       for (int e = 0; e < 4; ++e) s_red[wave][(nb * NW + m) * 4 + e][lane] = acc[nb][m][e];
   __syncthreads();
+  if (wave >= 4) return;
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     float v[NW];
 #pragma unroll
     for (int m = 0; m < NW; ++m) {
       const int at = (nb * NW + m) * 4 + wave;
-      v[m] = ((s_red[0][at][lane] + s_red[1][at][lane]) + s_red[2][at][lane]) + s_red[3][at][lane];
+      v[m] = s_red[0][at][lane];
+#pragma unroll
+      for (int k = 1; k < WAVES; ++k) v[m] += s_red[k][at][lane];
     }
     const int token = ti.m0 + c * 4 + wave, col = (unit0 + nb) * kUnit + r;
     if (token < ti.rows && col < a.g.N) {
@@ -382,13 +384,13 @@ __device__ __forceinline__ void split_product(const Args& a, const TileInfo& ti,
   }
 }
 
-template <int NB, int NW, int G, bool ZERO, bool F32, int kRing>
-__global__ __launch_bounds__(256, 2) void w4_gemm(const Args first, const Args second, const int b_blocks) {
+template <int NB, int NW, int G, bool ZERO, bool F32, int kRing, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void w4_gemm(const Args first, const Args second, const int b_blocks) {
   __shared__ Place s_place;
-  __shared__ float s_red[4][NB * NW * 4][64];
+  __shared__ float s_red[WAVES][NB * NW * 4][64];
   const Place place = find_place<16>(first, second, b_blocks, NB, 16, NB, &s_place);
   if (place.ti.group < 0) return;
-  split_product<NB, NW, G, ZERO, F32, kRing>((int)blockIdx.x < b_blocks ? second : first, place.ti, place.matrix, place.cb * NB, s_red);
+  split_product<NB, NW, G, ZERO, F32, kRing, WAVES>((int)blockIdx.x < b_blocks ? second : first, place.ti, place.matrix, place.cb * NB, s_red);
 }
 
 // The same product for more rows: the four waves of a workgroup take NB units each over the whole K, and share x: a K block of it
@@ -617,7 +619,7 @@ __global__ __launch_bounds__(256, kRing == 1 ? 2 : 4) void w4_tile_gemm(const Ar
   if constexpr (SPLIT) {
     if (is_second) {
       static_assert(sizeof(float[4][SPLIT * NW * 4][64]) <= sizeof(s_x), "the sums fit where x would be");
-      split_product<SPLIT, NW, G, ZERO, false, 3>(second, ti, place.matrix, place.cb * SPLIT,
+      split_product<SPLIT, NW, G, ZERO, false, 3, 4>(second, ti, place.matrix, place.cb * SPLIT,
                                                   reinterpret_cast<float (*)[SPLIT * NW * 4][64]>(s_x));
       return;
     }
@@ -796,7 +798,7 @@ static int grid_for(long long threads) {
 }
 
 // TILE: w4_tile_gemm, whose workgroups have 4 * NB units (SPLIT: of the second problem one); else w4_gemm with NB
-template <bool TILE, int MT, int NB, int NW, bool F32, int RING, int SPLIT = 0>
+template <bool TILE, int MT, int NB, int NW, bool F32, int RING, int SPLIT = 0, int WAVES = 4>
 static int launch_typed(const Args& a, const Args* b, int group, bool zeros, int total_rows, hipStream_t s) {
   constexpr int BM = 16 * MT, UNITS = TILE ? 4 * NB : NB, B_ROWS = SPLIT ? 16 : BM, B_UNITS = SPLIT ? SPLIT : UNITS;
   const int n_cb = ((a.g.N + kUnit - 1) / kUnit + UNITS - 1) / UNITS;
@@ -812,7 +814,7 @@ static int launch_typed(const Args& a, const Args* b, int group, bool zeros, int
 #define OCC_W4_CASE(G_, Z_)                                                                                                \
   if (group == kBlockK / G_ && zeros == Z_) {                                                                              \
     if constexpr (TILE) w4_tile_gemm<MT, NB, NW, G_, Z_, RING, SPLIT><<<(int)grid, 256, 0, s>>>(a, second, (int)b_blocks);        \
-    else w4_gemm<NB, NW, G_, Z_, F32, RING><<<(int)grid, 256, 0, s>>>(a, second, (int)b_blocks);                                 \
+    else w4_gemm<NB, NW, G_, Z_, F32, RING, WAVES><<<(int)grid, 64 * WAVES, 0, s>>>(a, second, (int)b_blocks);                                 \
     OCC_LAUNCH_CHECK(TILE ? "w4_tile_gemm" : "w4_gemm");                                                                   \
     return OCCULT_OK;                                                                                                      \
   }
@@ -836,8 +838,10 @@ static int launch(const occult_cfg_t& c, const Args& a, const Args* b, int group
   // 13.0 us (60 experts), 2 tokens 10.9 against 15.8 (64, none shared), 3 tokens 15.5 against 18.9 (64, 6 per token, 2 shared: 440
   // workgroups); equal from 6 tokens on (60: 616).  Down: 2 tokens 10.0 against 15.0 (64, 2 shared: 416), 3 tokens 11.0 against 17.2 (608).
   const long long tiles = min_i(rows, rows / 16 + c.E) + (b ? (long long)b->g.ngroups * ((c.T + 15) / 16) : 0);
+  // Eight waves for the down product, which may have a long sum over shared experts beside short ones (1 token, 4 shared 8.8 against 10.6 us
+  // with four, 2 tokens 9.4 against 10.9; none shared 5.9 against 6.0); four for gate/up (2 tokens 10.5 against 11.1).
   if (tiles * ((a.g.N + 4 * kUnit - 1) / (4 * kUnit)) <= 640)
-    return launch_typed<false, 1, 1, NW, false, NW == 2 ? 2 : 4>(a, b, group, zeros, rows, s);
+    return launch_typed<false, 1, NW == 2 ? 1 : 2, NW, false, 2, 0, NW == 2 ? 4 : 8>(a, b, group, zeros, rows, s);
   const long long per_expert = rows / c.E;
   if constexpr (NW == 1) {
     // A long sum over the shared experts' matrices beside short routed ones (K blocks: 44 of 4 shared experts, 22 of 2): 4 tokens split 12.2
