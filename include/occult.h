@@ -277,7 +277,8 @@ int occult_expert_ffn_packed(const occult_cfg_t* cfg, const occult_plan_t* plan,
  *   matrix 64 pieces of 16 bytes, piece l = row l % 16, whose dword j holds K elements j * 32 + (l / 16) * 8 .. + 8: element 2i in bits
  *   4i .. 4i + 3, 2i + 1 in bits 16 + 4i .., rotated left by 3.  Scales follow the codes of all matrices in the same order.
  * occult_expert_ffn_w4 is occult_expert_ffn computed from them: same plan, same rows, same outputs; products of x and codes are
- *   summed in f32 per group and scaled in f32 (f32 layers: x is not rounded either); h is rounded to cfg.dtype between the
+ *   summed in f32 per group and scaled in f32 (f32 layers: x is not rounded either; a row of x with an infinity or NaN gives
+ *   non-finite rows, of either kind); h is rounded to cfg.dtype between the
  *   two products.  cfg.ffn_phase as there.  Which kernel computes a product, and with it the last bits, depends on T, E, k, S, d and
  *   f; for one layer description results are the same bits every time.  A launch of 2^24 workgroups or more is refused (OCCULT_ESHAPE).
  * occult_forward_w4 is occult_forward with occult_expert_ffn_w4 in the place of the expert computation (no pre-activations

@@ -5,7 +5,7 @@
 //
 // The products are bound by streaming the active experts' codes (half a byte per weight, against two in bf16), with the vector
 // instructions that turn codes into matrix operands next: v_mfma_f32_16x16x32_bf16 wants 8 bf16 per lane.  Two codes at a time are
-// put, by a rotation and one and-or, into the mantissas of bf16 numbers in [16, 32): the operand is 16 + code exactly, 7
+// put, by a shift and one and-or, into the mantissas of bf16 numbers in [16, 32): the operand is 16 + code exactly, 7
 // instructions per 8 weights.  What is too much, (16 + zero) * sum x, is itself a matrix product with a constant operand, whose result
 // is where the accumulation of a group starts; a group's f32 sum is then scaled once, in f32, by the scale of the lane's own weight
 // row (weights are the column operand: an accumulator's lane has one weight row).  No weight is rounded on the way.
@@ -608,6 +608,7 @@ __device__ __forceinline__ void tile_product(const Args& a, const TileInfo& ti, 
 template <int MT, int NB, int NW, int G, bool ZERO, int kRing, int SPLIT>
 __global__ __launch_bounds__(256, kRing == 1 ? 2 : 4) void w4_tile_gemm(const Args first, const Args second, const int b_blocks) {
   constexpr int BM = 16 * MT;
+  static_assert(MT <= 2, "one or two blocks of rows");
   static_assert(kRing == 1 || kRing % 2 == 0, "the LDS buffers alternate");
   __shared__ Place s_place;
   constexpr int kLds = 2 * BM * kPitch > SPLIT * NW * 4096 ? 2 * BM * kPitch : SPLIT * NW * 4096;
@@ -628,7 +629,6 @@ __global__ __launch_bounds__(256, kRing == 1 ? 2 : 4) void w4_tile_gemm(const Ar
   const int unit0 = (place.cb * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * NB;
   const int left = ti.rows - ti.m0;   // a tile's empty blocks of 16 rows are not multiplied
   if (MT == 1 || left <= 16) tile_product<1, NB, NW, G, ZERO, kRing>(a, ti, place.matrix, unit0, s_x);
-  else if (MT == 2 || left <= 32) tile_product<(MT < 2 ? MT : 2), NB, NW, G, ZERO, kRing>(a, ti, place.matrix, unit0, s_x);
   else tile_product<MT, NB, NW, G, ZERO, kRing>(a, ti, place.matrix, unit0, s_x);
 }
 
@@ -797,7 +797,7 @@ static int grid_for(long long threads) {
   return (int)(blocks < 16384 ? blocks : 16384);
 }
 
-// TILE: w4_tile_gemm, whose workgroups have 4 * NB units (SPLIT: of the second problem one); else w4_gemm with NB
+// TILE: w4_tile_gemm, whose workgroups have 4 * NB units (of the second problem SPLIT, if not 0); else w4_gemm with NB
 template <bool TILE, int MT, int NB, int NW, bool F32, int RING, int SPLIT = 0, int WAVES = 4>
 static int launch_typed(const Args& a, const Args* b, int group, bool zeros, int total_rows, hipStream_t s) {
   constexpr int BM = 16 * MT, UNITS = TILE ? 4 * NB : NB, B_ROWS = SPLIT ? 16 : BM, B_UNITS = SPLIT ? SPLIT : UNITS;
@@ -813,16 +813,16 @@ static int launch_typed(const Args& a, const Args* b, int group, bool zeros, int
   const Args& second = b ? *b : a;
 #define OCC_W4_CASE(G_, Z_)                                                                                                \
   if (group == kBlockK / G_ && zeros == Z_) {                                                                              \
-    if constexpr (TILE) w4_tile_gemm<MT, NB, NW, G_, Z_, RING, SPLIT><<<(int)grid, 256, 0, s>>>(a, second, (int)b_blocks);        \
-    else w4_gemm<NB, NW, G_, Z_, F32, RING, WAVES><<<(int)grid, 64 * WAVES, 0, s>>>(a, second, (int)b_blocks);                                 \
+    if constexpr (TILE) w4_tile_gemm<MT, NB, NW, G_, Z_, RING, SPLIT><<<(int)grid, 256, 0, s>>>(a, second, (int)b_blocks); \
+    else w4_gemm<NB, NW, G_, Z_, F32, RING, WAVES><<<(int)grid, 64 * WAVES, 0, s>>>(a, second, (int)b_blocks);             \
     OCC_LAUNCH_CHECK(TILE ? "w4_tile_gemm" : "w4_gemm");                                                                   \
     return OCCULT_OK;                                                                                                      \
   }
   OCC_W4_CASE(1, false)
-  OCC_W4_CASE(4, false)
-  OCC_W4_CASE(2, true)
   OCC_W4_CASE(2, false)
+  OCC_W4_CASE(4, false)
   OCC_W4_CASE(1, true)
+  OCC_W4_CASE(2, true)
   OCC_W4_CASE(4, true)
 #undef OCC_W4_CASE
   OCC_FAIL(OCCULT_EINVAL, "group=%d", group);
