@@ -43,7 +43,7 @@ struct BackwardArgs {
 };
 
 // waves of a workgroup: at least 4 in the forward pass; 8 in the backward pass, whose workgroups each leave a set of column sums
-constexpr int block_waves(int W, bool backward) { return backward ? (W <= 8 ? 8 : W) : (W <= 4 ? 4 : W); }
+constexpr int block_waves(int W, bool backward) { return backward ? 8 : W <= 4 ? 4 : W; }
 
 // Which lanes hold which rows.  V vectors per lane, W waves per row.
 template <int V, int W, bool BACKWARD>
@@ -295,11 +295,31 @@ __global__ __launch_bounds__(64 * block_waves(W, true)) void block_norm_backward
   const int rows = P::rows_per_block(a.lanes);
   int slot = 0;
 
+  // With four vectors per lane, or two of bf16 and five column sums, the parameters are read again for every row (from L2) and no row is
+  // requested ahead: kept in registers both would spill (2195 rows of 7640 f32: 298 us, so 76; 2048 of 5000 bf16 69.6, so 61.8).
+  constexpr bool kTight = V == 4 || (V == 2 && LAYER && BF16);
   RowRegs<BF16, V> post_w, post_b, pre_w, cgate;
-  post_w.load_channels(a.post_w, a.row_vecs, p.lane, p.stride);
-  post_b.load_channels(a.post_b, a.row_vecs, p.lane, p.stride);
-  pre_w.load_channels(a.pre_w, a.row_vecs, p.lane, p.stride);
-  cgate.load_channels(a.gate_kind == OCCULT_GATE_CHANNEL ? a.gate : nullptr, a.row_vecs, p.lane, p.stride);
+  const void* const gate_channels = a.gate_kind == OCCULT_GATE_CHANNEL ? a.gate : nullptr;
+  if constexpr (!kTight) {
+    post_w.load_channels(a.post_w, a.row_vecs, p.lane, p.stride);
+    post_b.load_channels(a.post_b, a.row_vecs, p.lane, p.stride);
+    pre_w.load_channels(a.pre_w, a.row_vecs, p.lane, p.stride);
+    cgate.load_channels(gate_channels, a.row_vecs, p.lane, p.stride);
+  }
+  // (loads and their unpacked values stay inside a phase of a row)
+  auto phase = [&]() {
+    if constexpr (kTight) asm volatile("" ::: "memory");
+  };
+  auto channels = [&](const RowRegs<BF16, V>& kept, const void* base, int i, float* v) {
+    if constexpr (kTight) {
+      const int c = p.lane + i * p.stride;
+      typename R::Raw raw{};
+      if (base && c < a.row_vecs) raw = static_cast<const typename R::Raw*>(base)[c];
+      R::unpack(raw, v);
+    } else {
+      kept.unpack(i, v);
+    }
+  };
   const bool need_y = a.dy && (a.post || a.gate_kind);
 
   float col[NS][V][NE];
@@ -327,16 +347,21 @@ __global__ __launch_bounds__(64 * block_waves(W, true)) void block_norm_backward
   };
   const long long step = (long long)gridDim.x * rows;
   Rows next;
-  load(next, (long long)blockIdx.x * rows);
+  if constexpr (!kTight) load(next, (long long)blockIdx.x * rows);
   for (long long t0 = (long long)blockIdx.x * rows; t0 < a.T; t0 += step) {
     const bool valid = t0 + p.row < a.T;
     const size_t t = valid ? t0 + p.row : 0;
-    post_w.keep_raw();
-    post_b.keep_raw();
-    pre_w.keep_raw();
-    cgate.keep_raw();
+    if constexpr (kTight) {
+      load(next, t0);
+    } else {
+      post_w.keep_raw();
+      post_b.keep_raw();
+      pre_w.keep_raw();
+      cgate.keep_raw();
+    }
     const Rows cur = next;
-    if (t0 + step < a.T) load(next, t0 + step);   // requested before this pass's sums, whose exchanges would otherwise leave memory idle
+    // requested before this pass's sums, whose exchanges would otherwise leave memory idle
+    if (!kTight && t0 + step < a.T) load(next, t0 + step);
     const RowRegs<BF16, V>&yr = cur.y, &outr = cur.out, &doutr = cur.dout, &dhr = cur.dh, &gr = cur.gate;
     const float token_gate = cur.token_gate;
 
@@ -374,7 +399,7 @@ __global__ __launch_bounds__(64 * block_waves(W, true)) void block_norm_backward
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       float w[NE], g[NE];
-      pre_w.unpack(i, w);
+      channels(pre_w, a.pre_w, i, w);
       dhr.unpack(i, g);
       weight_of<NE>(a.pre_w != nullptr, a.offset, w);
 #pragma unroll
@@ -386,13 +411,14 @@ __global__ __launch_bounds__(64 * block_waves(W, true)) void block_norm_backward
       }
     }
     row_sums<W, P::kWaves>(s, a.lanes, slot);
+    phase();
     if (a.pre) {
       const float r = 1.0f / sqrtf(fmaf(s[0], a.inv_d, a.pre_eps));
       const float m2 = s[2] * r * a.inv_d, m1 = LAYER && a.pre == OCCULT_NORM_LAYER ? s[3] * a.inv_d : 0.0f;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         float w[NE], g[NE];
-        pre_w.unpack(i, w);
+        channels(pre_w, a.pre_w, i, w);
         dhr.unpack(i, g);
         weight_of<NE>(a.pre_w != nullptr, a.offset, w);
 #pragma unroll
@@ -404,6 +430,7 @@ __global__ __launch_bounds__(64 * block_waves(W, true)) void block_norm_backward
         }
       }
     }
+    phase();
     if (a.dx) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
@@ -415,6 +442,7 @@ __global__ __launch_bounds__(64 * block_waves(W, true)) void block_norm_backward
       }
     }
     if (!a.dy) continue;   // uniform over the grid
+    phase();
     const float r = a.post ? 1.0f / sqrtf(fmaf(s[1], a.inv_d, a.post_eps)) : 1.0f;
     // D becomes q = dz * w, the gradient of the normalised row; sums of the post norm's gradient and of a token's gate
     float u[3] = {0.0f, 0.0f, 0.0f};
@@ -423,10 +451,10 @@ __global__ __launch_bounds__(64 * block_waves(W, true)) void block_norm_backward
       const int c = p.lane + i * p.stride;
       const bool in = c < a.row_vecs;
       float w[NE], b[NE], g[NE], dg[NE];
-      post_w.unpack(i, w);
-      post_b.unpack(i, b);
+      channels(post_w, a.post_w, i, w);
+      channels(post_b, a.post_b, i, b);
       weight_of<NE>(a.post_w != nullptr, a.offset, w);
-      if (a.gate_kind == OCCULT_GATE_CHANNEL) cgate.unpack(i, g);
+      if (a.gate_kind == OCCULT_GATE_CHANNEL) channels(cgate, gate_channels, i, g);
       else if (a.gate_kind == OCCULT_GATE_ELEMENT) gr.unpack(i, g);
       else
 #pragma unroll
@@ -448,6 +476,7 @@ __global__ __launch_bounds__(64 * block_waves(W, true)) void block_norm_backward
     }
     if (a.post || a.gate_kind == OCCULT_GATE_TOKEN) row_sums<W, P::kWaves>(u, a.lanes, slot);
     if (a.gate_kind == OCCULT_GATE_TOKEN && a.dgate && valid && p.lane == 0) static_cast<float*>(a.dgate)[t] = u[2];
+    phase();
     const float m2 = a.post ? u[0] * a.inv_d : 0.0f, m1 = LAYER && a.post == OCCULT_NORM_LAYER ? u[1] * a.inv_d : 0.0f;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -528,7 +557,8 @@ __global__ __launch_bounds__(1024) void column_sums_kernel(const ColumnArgs a) {
 // Vectors per lane, waves per row and lanes per row of a row length: V and W of the kernels above.  Forward: two vectors per lane before a
 // second wave (16384 rows of 2048 bf16: 47 us, with one 51, with four 51; one row 3.3, 2.8, 4.6).  Backward: one vector per lane up to eight
 // waves (the column sums take registers: 1000 rows of 2048 12.8 us, with two 15.8; 16384 rows the same 76, with
-// means and biases 92 against 126), two beyond.
+// means and biases 92 against 126), then two and four (sixteen waves of two leave 128 registers: 2195 rows of 7640 f32 134 us, eight
+// of four 75; 2048 rows of 16384 bf16 299 and 209, both of which spill).
 struct Shape {
   int V, W, lanes;
 };
@@ -538,8 +568,8 @@ static Shape shape_of(int row_vecs, bool backward) {
     while (s.lanes > 1 && s.lanes / 2 >= row_vecs) s.lanes /= 2;
     return s;
   }
-  if (!backward || row_vecs > 512) s.V = 2;
-  while (64 * s.V * s.W < row_vecs) s.W *= 2;   // rows up to kMaxRowBytes: 16 waves of 2
+  s.V = !backward ? 2 : row_vecs <= 512 ? 1 : row_vecs <= 1024 ? 2 : 4;
+  while (64 * s.V * s.W < row_vecs) s.W *= 2;   // rows up to kMaxRowBytes: 16 waves of 2, 8 of 4
   return s;
 }
 static int rows_per_block(const Shape& s, bool backward) {
@@ -626,7 +656,7 @@ static int launch_backward(const BackwardArgs& a, const Shape& s, int grid, hipS
   OCC_NORM_CASE(1, 4)
   OCC_NORM_CASE(1, 8)
   OCC_NORM_CASE(2, 8)
-  OCC_NORM_CASE(2, 16)
+  OCC_NORM_CASE(4, 8)
 #undef OCC_NORM_CASE
   OCC_FAIL(OCCULT_ESHAPE, "no kernel for rows of %d vectors", a.row_vecs);
 }
