@@ -42,8 +42,11 @@ struct BackwardArgs {
   float x_scale, y_scale, post_eps, pre_eps, offset, inv_d;
 };
 
-// waves of a workgroup: at least 4 in the forward pass; 8 in the backward pass, whose workgroups each leave a set of column sums
-constexpr int block_waves(int W, bool backward) { return backward ? 8 : W <= 4 ? 4 : W; }
+// Waves of a workgroup, a multiple of those of a row: at least 4 in the forward pass, about 8 in the backward pass, whose workgroups each
+// leave a set of column sums.
+constexpr int block_waves(int W, bool backward) {
+  return backward ? (W == 3 ? 9 : W == 5 ? 10 : 8) : W <= 4 ? 4 : W;
+}
 
 // Which lanes hold which rows.  V vectors per lane, W waves per row.
 template <int V, int W, bool BACKWARD>
@@ -489,8 +492,11 @@ __global__ __launch_bounds__(64 * block_waves(W, true)) void block_norm_backward
   }
 
   if (!a.sums) return;
-  constexpr int kThreads = P::kWaves * 64;
-  __shared__ float s_col[W < P::kWaves ? kThreads * V * NE : 1];   // unused where a workgroup has one row at a time
+  // A wave's row groups are added across its lanes, then the workgroup's waves (W == 1) or rows through LDS in their order.
+  constexpr int kGroups = W == 1 ? P::kWaves : P::kWaves / W;
+  const int wave = threadIdx.x >> 6, group = W == 1 ? wave : p.row;
+  const bool leads = W > 1 || (int)(threadIdx.x & 63) < a.lanes;   // one of its wave's row groups
+  __shared__ float s_col[kGroups > 1 ? P::kWaves * 64 * V * NE : 1];
   const int d = a.row_vecs * NE;
   float* ws = a.ws + (size_t)blockIdx.x * __popc(a.sums) * d;
 #pragma unroll
@@ -498,21 +504,31 @@ __global__ __launch_bounds__(64 * block_waves(W, true)) void block_norm_backward
     // bits of `sums`: post weight, post bias, pre weight, pre bias, channel gate
     constexpr int kBit[kColSums] = {0, 2, 4, 1, 3};
     if (!(a.sums >> kBit[n] & 1)) continue;   // uniform
-    float* mine = s_col + (p.row * p.stride + p.lane) * V * NE;
-    __syncthreads();
-    if (p.row > 0) {
+    if constexpr (W == 1) {
+      for (int o = a.lanes; o < 64; o <<= 1)
 #pragma unroll
-      for (int i = 0; i < V; ++i)
+        for (int i = 0; i < V; ++i)
 #pragma unroll
-        for (int e = 0; e < NE; ++e) mine[i * NE + e] = col[n][i][e];
+          for (int e = 0; e < NE; ++e) col[n][i][e] += __shfl_xor(col[n][i][e], o, 64);
     }
-    __syncthreads();
-    if (p.row == 0) {
+    if constexpr (kGroups > 1) {
+      __syncthreads();
+      if (group > 0 && leads) {
+        float* mine = s_col + (group * p.stride + p.lane) * V * NE;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+#pragma unroll
+          for (int e = 0; e < NE; ++e) mine[i * NE + e] = col[n][i][e];
+      }
+      __syncthreads();
+    }
+    if (group == 0 && leads) {
       float* dst = ws + (size_t)__popc(a.sums & ((1 << kBit[n]) - 1)) * d;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const int c = p.lane + i * p.stride;
-        for (int g = 1; g < rows; ++g)
+#pragma unroll
+        for (int g = 1; g < kGroups; ++g)
 #pragma unroll
           for (int e = 0; e < NE; ++e) col[n][i][e] += s_col[(g * p.stride + p.lane) * V * NE + i * NE + e];
         if (c < a.row_vecs)
@@ -570,6 +586,10 @@ static Shape shape_of(int row_vecs, bool backward) {
   }
   s.V = !backward ? 2 : row_vecs <= 512 ? 1 : row_vecs <= 1024 ? 2 : 4;
   while (64 * s.V * s.W < row_vecs) s.W *= 2;   // rows up to kMaxRowBytes: 16 waves of 2, 8 of 4
+  // Powers of two alone leave up to half of a row's lanes idle: backward 16384 rows of 1032 bf16 92 us, on three waves 81; 12000 of 2056
+  // 104, on five 72; six gain nothing (3000: 107 and 109), and forward three lose (60000 rows of 2056 241 us, 303).
+  if (backward && s.V == 1 && s.W == 4 && row_vecs <= 192) s.W = 3;
+  if (backward && s.V == 1 && s.W == 8 && row_vecs <= 320) s.W = 5;
   return s;
 }
 static int rows_per_block(const Shape& s, bool backward) {
@@ -653,7 +673,9 @@ static int launch_backward(const BackwardArgs& a, const Shape& s, int grid, hipS
   }
   OCC_NORM_CASE(1, 1)
   OCC_NORM_CASE(1, 2)
+  OCC_NORM_CASE(1, 3)
   OCC_NORM_CASE(1, 4)
+  OCC_NORM_CASE(1, 5)
   OCC_NORM_CASE(1, 8)
   OCC_NORM_CASE(2, 8)
   OCC_NORM_CASE(4, 8)

@@ -70,7 +70,7 @@ def check(norm, t, p, th, ph, cfg, what):
 
 
 # rows of one vector, of part of a wave, of several vectors per lane, of several waves; odd numbers of vectors
-@pytest.mark.parametrize("d", [8, 64, 72, 264, 520, 1000, 1032, 2048, 2056, 4104, 8192, 16384])
+@pytest.mark.parametrize("d", [8, 64, 72, 264, 520, 1000, 1032, 1536, 1600, 2048, 2056, 2560, 2568, 4104, 8192, 16384])
 @pytest.mark.parametrize("kind", ["rms", "layer"])
 def test_row_lengths(d, kind):
     for T in (1, 3, 70):
