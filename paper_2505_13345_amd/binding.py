@@ -495,9 +495,10 @@ def occult_forward_w4(cfg, plan, logits, x, packed, group, zeros, ids, w, plan_w
     buf = occult_forward_buffers_t(_ptr(ids), _ptr(w), _ptr(plan_ws), _ptr(sfd_x), _ptr(epd_h), _ptr(epd_y), _ptr(h_shared),
                                    _ptr(y_shared), None, None, None, _ptr(sfd_y), _ptr(y),
                                    plan_ws.numel() * plan_ws.element_size(), 0)
+    s = _stream_of(x.get_device()) if stream is None and x is not None and x.is_cuda else _stream(stream)
     _check(load_library().occult_forward_w4(ctypes.byref(cfg), ctypes.byref(plan), _ptr(logits), _ptr(x), _ptr(packed),
                                             packed.numel() * packed.element_size(), int(group), int(bool(zeros)), ctypes.byref(buf),
-                                            _stream(stream)))
+                                            s))
 
 
 def make_block_norm(post_kind, pre_kind, gate_kind, x_scale=1.0, y_scale=1.0, post_eps=1e-6, pre_eps=1e-6, weight_offset=0.0,

@@ -629,7 +629,7 @@ static int check(const occult_cfg_t* cfg, const occult_block_norm_t* n) {
   OCC_REQUIRE((n->gate != nullptr) == (n->gate_kind != OCCULT_GATE_NONE) || c.T == 0, OCCULT_ENULLPTR,
               "gate and gate_kind=%d do not belong together", n->gate_kind);
   OCC_REQUIRE(aligned16(n->post_weight) && aligned16(n->post_bias) && aligned16(n->pre_weight) && aligned16(n->pre_bias) &&
-                  (n->gate_kind == OCCULT_GATE_TOKEN || aligned16(n->gate)),
+                  (n->gate_kind == OCCULT_GATE_TOKEN ? (uintptr_t)n->gate % elem_size(c) == 0 : aligned16(n->gate)),
               OCCULT_EALIGN, "a parameter is not 16-byte aligned");
   return OCCULT_OK;
 }

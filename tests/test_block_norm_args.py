@@ -39,7 +39,7 @@ def backward(lib, n, c=None, y=P, out=2 * P, dout=3 * P, dh=4 * P, dx=5 * P, dy=
     (dict(post_eps=0.0), -1), (dict(pre_eps=-1e-6), -1), (dict(pre_eps=float("inf")), -1),
     (dict(post_kind=0, post_weight=P), -1), (dict(pre_kind=0, pre_bias=P), -1),
     (dict(gate_kind=1), -4), (dict(gate=P), -4),
-    (dict(post_weight=P + 8), -3), (dict(gate_kind=3, gate=P + 2), -3)])
+    (dict(post_weight=P + 8), -3), (dict(gate_kind=3, gate=P + 2), -3), (dict(gate_kind=2, gate=P + 1), -3)])
 def test_descriptions_that_do_not_hold_together(lib, kw, code):
     assert forward(lib, desc(**kw)) == code
     assert backward(lib, desc(**kw)) == code

@@ -119,6 +119,23 @@ def test_more_rows_than_one_pass_of_the_grid():
         assert torch.equal(one[0], out[i]) and torch.equal(one_h[0], h[i]), i   # a token's results do not depend on T
 
 
+def test_rows_beyond_4_gib():
+    """Buffers of 4.4 GB: the first, middle and last rows against a call on those rows alone (a token's bits do not depend on T)."""
+    dev = require_gpu()
+    T, d = 270_000, 8192
+    pick = [0, 1, T // 2, 262_143, 262_144, T - 1]
+    gen = torch.Generator(device=dev).manual_seed(4)
+    x, y, dout, dh = (torch.randn((T, d), device=dev, generator=gen, dtype=torch.bfloat16) for _ in range(4))
+    w = torch.randn(d, device=dev, generator=gen, dtype=torch.bfloat16)
+    big, small = BlockNorm(T, d, post="rms", pre="rms"), BlockNorm(len(pick), d, post="rms", pre="rms")
+    out, h = big.forward(x, y, post_weight=w, pre_weight=w)
+    some, some_h = small.forward(x[pick], y[pick], post_weight=w, pre_weight=w)
+    assert torch.equal(out[pick], some) and torch.equal(h[pick], some_h)
+    g = big.backward(out, dout, dh, y, post_weight=w, pre_weight=w)
+    part = small.backward(some, dout[pick], dh[pick], y[pick], post_weight=w, pre_weight=w)
+    assert torch.equal(g["dx"][pick], part["dx"]) and torch.equal(g["dy"][pick], part["dy"])
+
+
 def test_pre_norm_alone():
     norm, t, p, th, ph, cfg = case(21, 1000, "bf16", None, "rms", None)
     same, h = norm.forward(t["x"], **p)

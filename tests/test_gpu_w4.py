@@ -155,6 +155,33 @@ def test_placed_experts_and_a_large_batch():
     check_network(layer, x, values, tops, "bf16", "placed")
 
 
+def test_rows_beyond_4_gib():
+    """x, sfd_x, epd_y and y_shared of 4.5 GB: rows at both ends and around the border against the oracle."""
+    dev = require_gpu()
+    T, d, f, E, S, k = 550_000, 4096, 64, 4, 1, 1
+    small = make(8, d, f, E, S, k, 1, "bf16", 128, True, seed=13)
+    values, tops = small[4], small[5]
+    layer = OccultLayer(T, d, f, E, S, k, 1)
+    layer.pack_weights_w4(small[3])
+    gen = torch.Generator(device=dev).manual_seed(5)
+    xd = torch.randn((T, d), device=dev, generator=gen, dtype=torch.bfloat16)
+    layer.route(torch.randn((T, E), device=dev, generator=gen))
+    layer.make_plan()
+    layer.dispatch(xd)
+    layer.expert_ffn_w4(xd)
+    offset = layer.tables()["exp_offset"].cpu().numpy()
+    src = layer.tables()["sfd_token"][layer.tables()["epd_sfd_row"].long()]
+    for row in (0, 1, 524_287, 524_288, T - 1):
+        e, t = int(np.searchsorted(offset, row, side="right") - 1), int(src[row])
+        for expert, rows, h, y in ((e, t, layer.epd_h[row], layer.epd_y[row]), (E, row, layer.h_shared[row], layer.y_shared[row])):
+            x = f64(xd[rows])
+            g, up = values[0][expert] @ x, values[1][expert] @ x
+            want = g / (1.0 + np.exp(-g)) * up
+            h = f64(h)
+            assert np.abs(h - want).max() <= 2 * BF16_U * np.abs(want).max(), (row, "h")
+            compare(f64(y), values[2][expert] @ h, np.abs(values[2][expert]) @ np.abs(h), tops[2][expert] @ np.abs(h), "bf16", f"row {row} y")
+
+
 def test_phases_and_rows_behind_the_last():
     """The two products one by one give the same bits; scratch rows behind the batch's stay as they were."""
     dev = require_gpu()
