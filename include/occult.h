@@ -470,10 +470,12 @@ int occult_expert_ffn_backward_weights_ws(const occult_cfg_t* cfg, const occult_
  * be x or y, but not each other; buffers that overlap in another way are not for this call.
  *
  * occult_block_norm_backward: from dout [T][d], the gradient of out from where it is read beside h (NULL = none; needed without a pre
- * norm), dh [T][d], the gradient of h, and y and out as the forward pass read and wrote them (for the pre norm alone: out = x, dy = NULL):
+ * norm), dh [T][d], the gradient of h, and y and out as the forward pass read and wrote them:
  *   D = dout + N_pre'(dh);   dx = x_scale * D;   dy = N_post'(y_scale * gate * D);   gate gradient = y_scale * N_post(y) * D
+ * The pre norm alone (forward without y): neither post norm nor gate, out = x, y = dy = NULL; then dx = D, for x_scale has no part in it.
  * dx, dy [T][d] in cfg.dtype, one of them may be NULL (dy: then no gradient of post norm or gate either); y may be NULL where there
- * is neither post norm nor gate.  grads: each NULL or the gradient of that parameter, f32 [d], summed over tokens
+ * is neither post norm nor gate and dy is wanted (where dy is not wanted, y is not read: any address but NULL says that there
+ * was one).  grads: each NULL or the gradient of that parameter, f32 [d], summed over tokens
  * (accumulate = 1: added to what is there); gate: CHANNEL f32 [d] likewise, TOKEN f32 [T] and ELEMENT [T][d] in cfg.dtype written
  * per token whatever accumulate is.  The sums over tokens go through ws (device ptr, 16-byte aligned,
  * >= occult_block_norm_backward_ws_bytes() bytes, contents not kept) in a fixed order, without atomics.  T == 0 writes zeros to the sums /

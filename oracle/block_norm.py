@@ -66,7 +66,8 @@ def pre_norm(out, cfg, p):
 
 
 def gradients(out, y, dout, dh, cfg, p):
-    """dict name -> (gradient, scale): dx, dy, dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias."""
+    """dict name -> (gradient, scale): dx, dy, dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias.  y = None: the pre norm alone,
+    h = N_pre(x) and out = x, in which x_scale has no part."""
     res = {}
     D = np.zeros_like(out) if dout is None else dout
     D_s = np.abs(D)
@@ -77,9 +78,10 @@ def gradients(out, y, dout, dh, cfg, p):
             res["dpre_weight"] = tuple(a.sum(axis=0) for a in dw)
         if "pre_bias" in p:
             res["dpre_bias"] = tuple(a.sum(axis=0) for a in db)
-    res["dx"] = (cfg["x_scale"] * D, np.abs(cfg["x_scale"]) * D_s)
     if y is None:
+        res["dx"] = (D, D_s)
         return res
+    res["dx"] = (cfg["x_scale"] * D, np.abs(cfg["x_scale"]) * D_s)
     z, z_s = norm(y, cfg["post"], cfg["post_eps"], p.get("post_weight"), p.get("post_bias"), cfg["offset"])
     ys = cfg["y_scale"]
     if cfg["gate"]:

@@ -2,6 +2,7 @@
 //
 //   forward   out = x_scale * x + y_scale * gate * N_post(y);   h = N_pre(out)
 //   backward  D = dout + N_pre'(dh);   dx = x_scale * D;   dz = y_scale * gate * D;   dy = N_post'(dz);   dgate = y_scale * z * D
+//   (without y, the pre norm alone: h = N_pre(x), dx = D)
 //   with N(v) = vh * w + b, vh = (v - mu) * r, r = 1 / sqrt(mean((v - mu)^2) + eps), mu = 0 (RMS) or mean(v) (LAYER), and
 //   N'(g) = r * (q - vh * mean(q * vh) - [LAYER] mean(q)), q = g * w.
 //
@@ -765,7 +766,9 @@ extern "C" int occult_block_norm_backward(const occult_cfg_t* cfg, const occult_
   a.ws = static_cast<float*>(ws);
   a.T = c.T; a.row_vecs = c.d * elem_size(c) / 16;
   a.post = n->post_kind; a.pre = n->pre_kind; a.gate_kind = n->gate_kind; a.sums = sums;
-  a.x_scale = n->x_scale; a.y_scale = n->y_scale; a.post_eps = n->post_eps; a.pre_eps = n->pre_eps;
+  // the pre norm alone: h = N_pre(x) has no x_scale in it
+  const bool alone = !y && !dy && n->post_kind == OCCULT_NORM_NONE && n->gate_kind == OCCULT_GATE_NONE;
+  a.x_scale = alone ? 1.0f : n->x_scale; a.y_scale = n->y_scale; a.post_eps = n->post_eps; a.pre_eps = n->pre_eps;
   a.offset = n->weight_offset; a.inv_d = 1.0f / (float)c.d;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (c.T > 0) {

@@ -87,14 +87,16 @@ class BlockNorm:
 
     def backward(self, out, dout, dh=None, y=None, gate=None, post_weight=None, post_bias=None, pre_weight=None, pre_bias=None,
                  accumulate=False, want_dy=None):
-        """out and y as the forward pass had them (y may be left out where there is neither post norm nor gate; want_dy then says
-        whether dy is wanted), dout the gradient of out from where it is read beside h (None = none), dh that
-        of h -> dict of dx, dy, dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias: each None where there is
+        """out and y as the forward pass had them, dout the gradient of out from where it is read beside h (None = none), dh that
+        of h.  Without y and want_dy: the pre norm alone (out = x; x_scale has no part in its dx).  Where there was a y, with
+        neither post norm nor gate, it may still be left out: want_dy then says whether dy is wanted -> dict of dx, dy, dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias: each None where there is
         nothing of that name; sums over tokens are f32 (accumulate: added to what the last call left)."""
         desc = self._describe(gate, post_weight, post_bias, pre_weight, pre_bias)
         T, d, f32 = self.T, self.d, torch.float32
         n = T * d
         rows = [self._at(t, name, n) for t, name in ((y, "y"), (out, "out"), (dout, "dout"), (dh, "dh"))]
+        if y is None and want_dy is not None and not want_dy:
+            rows[0] = rows[1] or rows[2]   # there was a y, which the call need not read
         want_dy = y is not None if want_dy is None else want_dy
         g = {"dx": self._buf("dx", (T, d), self.tdtype), "dy": self._buf("dy", (T, d), self.tdtype) if want_dy else None,
              "dpost_weight": self._buf("dpost_weight", (d,), f32) if post_weight is not None and want_dy else None,
