@@ -21,7 +21,9 @@ _GATES = {None: B.OCCULT_GATE_NONE, "channel": B.OCCULT_GATE_CHANNEL, "token": B
 class BlockNorm:
     """post, pre: "rms", "layer" or None (no norm there); gate: "channel" ([d]), "token" ([T]), "element" ([T, d]) or None.
     Parameters are passed to the calls: weights and biases [d] and the gate in the layer's type, each may be left out
-    (factor 1, summand 0; a gate that the kind asks for has to be there)."""
+    (factor 1, summand 0; a gate that the kind asks for has to be there).  One object may serve several blocks, threads and
+    streams with forward() calls that bring their own out and h; backward() calls share its buffers and workspace, and so
+    have to be in one order: one stream, or streams and graphs that wait for each other."""
 
     def __init__(self, T, d, dtype="bf16", post=None, pre="rms", gate=None, x_scale=1.0, y_scale=1.0, post_eps=1e-6, pre_eps=1e-6,
                  weight_offset=0.0, device="cuda:0"):
@@ -39,7 +41,7 @@ class BlockNorm:
         self._fixed = (_NORMS[post], _NORMS[pre], _GATES[gate], x_scale, y_scale, post_eps, pre_eps, weight_offset)
         self._gate_len = {None: 0, "channel": d, "token": T, "element": T * d}[gate]
         B.occult_block_norm_backward_ws_bytes(self.cfg, B.make_block_norm(_NORMS[post], _NORMS[pre], 0, *self._fixed[3:]))  # checks both
-        self.desc = B.make_block_norm(*self._fixed)   # its parameters are set by every call
+        self._desc = bytes(B.make_block_norm(*self._fixed))   # what every call's own description starts from
         self.out = torch.zeros((T, d), dtype=self.tdtype, device=self.device)
         self.h = torch.zeros((T, d), dtype=self.tdtype, device=self.device)
         self.ws = None
@@ -58,7 +60,8 @@ class BlockNorm:
     def _describe(self, gate, post_weight, post_bias, pre_weight, pre_bias):
         if torch.cuda.current_device() != self.device.index:   # the library launches on the current device's stream
             raise ValueError(f"occult: the current device is cuda:{torch.cuda.current_device()}, the buffers are on {self.device}")
-        desc, d = self.desc, self.d
+        # of this call alone: the library reads it while other threads may call this object
+        desc, d = B.occult_block_norm_t.from_buffer_copy(self._desc), self.d
         desc.post_weight = self._at(post_weight, "post_weight", d)
         desc.post_bias = self._at(post_bias, "post_bias", d)
         desc.pre_weight = self._at(pre_weight, "pre_weight", d)
