@@ -3,8 +3,8 @@
     out = x_scale * x + y_scale * gate * N_post(y);   h = N_pre(out)
 
 ``y`` is the block's output (``OccultLayer.forward``'s), ``x`` the residual stream in front of it, ``h`` the input of
-the next block.  Memory plumbing only, like layer.py: buffers are allocated once (the backward pass's on first use), a
-call is one call into the C library on the current stream, and nothing here synchronises or computes.
+the next block.  Memory plumbing only, like layer.py: buffers are allocated once (the backward pass's [T, d] and its workspace on
+first use), a call is one call into the C library on the current stream, and nothing here synchronises or computes.
 """
 from __future__ import annotations
 
@@ -44,8 +44,13 @@ class BlockNorm:
         self._desc = bytes(B.make_block_norm(*self._fixed))   # what every call's own description starts from
         self.out = torch.zeros((T, d), dtype=self.tdtype, device=self.device)
         self.h = torch.zeros((T, d), dtype=self.tdtype, device=self.device)
-        self.ws = None
-        self.dx = self.dy = self.dgate = self.dpost_weight = self.dpost_bias = self.dpre_weight = self.dpre_bias = None
+        self.ws = self.dx = self.dy = self.dgate = None
+        # Sums over tokens, which a backward call may add to: zeros from here on, as a fill inside that call would become part of a
+        # graph that is captured from it and clear them with every replay.
+        self.dpost_weight, self.dpost_bias, self.dpre_weight, self.dpre_bias, channel = torch.zeros(
+            (5, d), dtype=torch.float32, device=self.device)
+        if gate == "channel":
+            self.dgate = channel
 
     def _at(self, t, name, numel):
         """Device address of a caller's tensor (None passes through), with binding's checks of it in one place: on small batches
@@ -82,9 +87,10 @@ class BlockNorm:
         return (x if y is None else out), h
 
     def _buf(self, name, shape, dtype):
+        """A buffer that every call with it overwrites, allocated on first use."""
         t = getattr(self, name)
         if t is None:
-            t = torch.zeros(shape, dtype=dtype, device=self.device)
+            t = torch.empty(shape, dtype=dtype, device=self.device)
             setattr(self, name, t)
         return t
 
@@ -102,13 +108,12 @@ class BlockNorm:
             rows[0] = rows[1] or rows[2]   # there was a y, which the call need not read
         want_dy = y is not None if want_dy is None else want_dy
         g = {"dx": self._buf("dx", (T, d), self.tdtype), "dy": self._buf("dy", (T, d), self.tdtype) if want_dy else None,
-             "dpost_weight": self._buf("dpost_weight", (d,), f32) if post_weight is not None and want_dy else None,
-             "dpost_bias": self._buf("dpost_bias", (d,), f32) if post_bias is not None and want_dy else None,
-             "dpre_weight": self._buf("dpre_weight", (d,), f32) if pre_weight is not None else None,
-             "dpre_bias": self._buf("dpre_bias", (d,), f32) if pre_bias is not None else None, "dgate": None}
+             "dpost_weight": self.dpost_weight if post_weight is not None and want_dy else None,
+             "dpost_bias": self.dpost_bias if post_bias is not None and want_dy else None,
+             "dpre_weight": self.dpre_weight if pre_weight is not None else None,
+             "dpre_bias": self.dpre_bias if pre_bias is not None else None, "dgate": None}
         if self.gate is not None and want_dy:
-            shape, dtype = {"channel": ((d,), f32), "token": ((T,), f32), "element": ((T, d), self.tdtype)}[self.gate]
-            g["dgate"] = self._buf("dgate", shape, dtype)
+            g["dgate"] = self._buf("dgate", (T,) if self.gate == "token" else (T, d), f32 if self.gate == "token" else self.tdtype)
         if self.ws is None:   # enough for every parameter
             full = B.make_block_norm(*self._fixed, *[self.h if k else None for k in (self.post, self.post, self.pre, self.pre, self.gate)])
             self.ws = torch.empty(max(4, B.occult_block_norm_backward_ws_bytes(self.cfg, full) // 4), dtype=f32, device=self.device)
