@@ -481,13 +481,14 @@ __global__ __launch_bounds__(64 * block_waves(W, true)) void block_norm_backward
     if (a.post || a.gate_kind == OCCULT_GATE_TOKEN) row_sums<W, P::kWaves>(u, a.lanes, slot);
     if (a.gate_kind == OCCULT_GATE_TOKEN && a.dgate && valid && p.lane == 0) static_cast<float*>(a.dgate)[t] = u[2];
     phase();
-    const float m2 = a.post ? u[0] * a.inv_d : 0.0f, m1 = LAYER && a.post == OCCULT_NORM_LAYER ? u[1] * a.inv_d : 0.0f;
+    const float m2 = u[0] * a.inv_d, m1 = LAYER && a.post == OCCULT_NORM_LAYER ? u[1] * a.inv_d : 0.0f;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int c = p.lane + i * p.stride;
       float v[NE];
 #pragma unroll
-      for (int e = 0; e < NE; ++e) v[e] = r * (D[i][e] - m1 - y[i][e] * r * m2);
+      for (int e = 0; e < NE; ++e)   // without a post norm no value of y is in it: 0 * y is not 0 for an infinity or NaN
+        v[e] = a.post ? r * (D[i][e] - m1 - y[i][e] * r * m2) : D[i][e];
       if (valid && c < a.row_vecs) R::store_round(a.dy, t, a.row_vecs, c, v);
     }
   }
