@@ -346,8 +346,8 @@ __global__ __launch_bounds__(64 * block_waves(W, true)) void block_norm_backward
     r.dh.load(a.dh, t, a.row_vecs, p.lane, p.stride, valid && a.pre);
     r.y.load(a.y, t, a.row_vecs, p.lane, p.stride, valid && need_y);
     r.gate.load(a.gate, t, a.row_vecs, p.lane, p.stride, valid && a.gate_kind == OCCULT_GATE_ELEMENT);
-    r.token_gate = 1.0f;
-    if (a.gate_kind == OCCULT_GATE_TOKEN) r.token_gate = load_scalar<BF16>(a.gate, t);
+    r.token_gate = 1.0f;   // also where there is no token: 0 * another one's infinity would go into the column sums
+    if (a.gate_kind == OCCULT_GATE_TOKEN && valid) r.token_gate = load_scalar<BF16>(a.gate, t);
   };
   const long long step = (long long)gridDim.x * rows;
   Rows next;
