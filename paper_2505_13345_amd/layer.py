@@ -189,14 +189,16 @@ class OccultLayer:
 
     def pack_weights_w4(self, w4):
         """4-bit weights in the order that expert_ffn_w4() and forward_w4() read (again after every change of the weights, which
-        are not read after this).  Weights of the same group and kind of zero points go to the same buffer, also under a captured
-        graph; another group or kind takes a new buffer, which only graphs captured afterwards read."""
+        are not read after this).  The layer keeps one buffer per group and kind of zero points: weights of a form go to that form's
+        buffer, which the graphs captured with it go on reading; the eager calls read what was packed last."""
         self._expect_w4(w4)
         form = (w4.group, w4.has_zeros)
-        packed = getattr(self, "packed_w4", None)
-        if packed is None or self.w4_format != form:
+        forms = self.__dict__.setdefault("_packed_forms", {})
+        packed = forms.get(form)
+        if packed is None:
             packed = torch.empty(B.occult_pack_w4_bytes(self.cfg, *form), dtype=torch.uint8, device=self.device)
         B.occult_pack_w4(self.cfg, *w4, packed)
+        forms[form] = packed   # kept: a captured graph holds its address
         self.packed_w4, self.w4_format = packed, form
         return packed
 
