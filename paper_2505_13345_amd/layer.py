@@ -162,6 +162,7 @@ class OccultLayer:
 
     def _expect_w4(self, w4):
         B.occult_pack_w4_bytes(self.cfg, w4.group, w4.has_zeros)   # refuses the group and the layer's rows
+        self._here(*w4.codes, *w4.scales, *(w4.zeros or ()))
         for i, ((n, rows, K, groups), name) in enumerate(zip(self._w4_shapes(w4.group), ("gate", "up", "down"))):
             B.expect(w4.codes[i], f"codes of {name}", torch.uint8, n * rows * K // 2)
             B.expect(w4.scales[i], f"scales of {name}", torch.bfloat16, n * rows * groups)
@@ -171,6 +172,7 @@ class OccultLayer:
     def quantize_weights(self, w_gate, w_up, w_down, group=128, zeros=False):
         """The layer's weights rounded to 4 bits with a scale (and, if asked for, a zero point) per `group` weights along K."""
         self._weights(w_gate, w_up, w_down)
+        self._here(w_gate, w_up, w_down)
         B.occult_pack_w4_bytes(self.cfg, group, zeros)
         shapes = self._w4_shapes(group)
         empty = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=self.device)
@@ -207,9 +209,14 @@ class OccultLayer:
             raise ValueError("occult: no 4-bit weights: call pack_weights_w4() first")
         return (self.packed_w4, *self.w4_format)
 
-    def _here(self, x):
-        if x.is_cuda and x.get_device() != torch.cuda.current_device():   # the library launches on the current device's stream
-            raise ValueError(f"occult: the current device is cuda:{torch.cuda.current_device()}, x is on {x.device}")
+    def _here(self, *tensors):
+        """The library launches on the current device's stream, and its kernels read this layer's buffers and the caller's tensors."""
+        at = self.ws.get_device()
+        if at != torch.cuda.current_device():
+            raise ValueError(f"occult: the current device is cuda:{torch.cuda.current_device()}, the layer's buffers are on cuda:{at}")
+        for t in tensors:
+            if t is not None and t.is_cuda and t.get_device() != at:
+                raise ValueError(f"occult: a tensor is on cuda:{t.get_device()}, the layer's buffers are on cuda:{at}")
 
     def expert_ffn_w4(self, x):
         """expert_ffn() from 4-bit weights -> epd_y, y_shared (None without shared experts)."""
@@ -232,7 +239,7 @@ class OccultLayer:
         s = self.shape
         B.expect(logits, "logits", torch.float32, s["T"] * s["E"])
         self._hidden(x, "x")
-        self._here(x)
+        self._here(x, logits)
         self.gu_saved = False
         B.occult_forward_w4(self.cfg, self.plan, logits, x, *self._packed_w4(), self.ids, self.w, self.ws, self.sfd_x, self.epd_h,
                             self.epd_y, self.h_shared, self.y_shared, self.sfd_y, self.y)
