@@ -1,4 +1,4 @@
-"""4-bit weights with group scales: rounding, values and the expert network computed from them, in float64.
+"""4-bit weights with group scales: rounding and the values that codes stand for, in float64.
 
 weight[k] = scale[k // group] * (code[k] - zero[k // group]); codes 0..15, two per byte along K (the lower k in the low bits)."""
 from __future__ import annotations
@@ -45,14 +45,3 @@ def unpack_bytes(packed):
 def values(codes, scales, zeros, group):
     at = np.arange(codes.shape[-1]) // group
     return (codes - zeros[..., at]) * scales[..., at]
-
-
-def network(x, w_gate, w_up, w_down, round_h=lambda h: h):
-    """One SwiGLU expert on rows x -> y, and the scale of y's error: sums of the magnitudes of its terms.  round_h: the rounding of the
-    stored intermediate."""
-    g, u = x @ w_gate.T, x @ w_up.T
-    h = round_h(g / (1.0 + np.exp(-g)) * u)
-    g_s, u_s = np.abs(x) @ np.abs(w_gate).T, np.abs(x) @ np.abs(w_up).T
-    # |silu'| <= 1.1 and |silu(g)| <= |g|
-    h_s = 1.1 * g_s * np.abs(u) + np.abs(g) * u_s
-    return h @ w_down.T, np.abs(h) @ np.abs(w_down).T, h_s @ np.abs(w_down).T

@@ -797,8 +797,9 @@ static int grid_for(long long threads) {
   return (int)(blocks < 16384 ? blocks : 16384);
 }
 
-// TILE: w4_tile_gemm, whose workgroups have 4 * NB units (of the second problem SPLIT, if not 0); else w4_gemm with NB
-template <bool TILE, int MT, int NB, int NW, bool F32, int RING, int SPLIT = 0, int WAVES = 4>
+// TILE: w4_tile_gemm, whose workgroups have 4 * NB units (of the second problem SPLIT, if not 0); else w4_gemm with NB.
+// MIN_GROUP: the finest groups that the caller's rule sends here.
+template <bool TILE, int MT, int NB, int NW, bool F32, int RING, int SPLIT = 0, int WAVES = 4, int MIN_GROUP = 32>
 static int launch_typed(const Args& a, const Args* b, int group, bool zeros, int total_rows, hipStream_t s) {
   constexpr int BM = 16 * MT, UNITS = TILE ? 4 * NB : NB, B_ROWS = SPLIT ? 16 : BM, B_UNITS = SPLIT ? SPLIT : UNITS;
   const int n_cb = ((a.g.N + kUnit - 1) / kUnit + UNITS - 1) / UNITS;
@@ -820,10 +821,12 @@ static int launch_typed(const Args& a, const Args* b, int group, bool zeros, int
   }
   OCC_W4_CASE(1, false)
   OCC_W4_CASE(2, false)
-  OCC_W4_CASE(4, false)
   OCC_W4_CASE(1, true)
   OCC_W4_CASE(2, true)
-  OCC_W4_CASE(4, true)
+  if constexpr (MIN_GROUP == 32) {
+    OCC_W4_CASE(4, false)
+    OCC_W4_CASE(4, true)
+  }
 #undef OCC_W4_CASE
   OCC_FAIL(OCCULT_EINVAL, "group=%d", group);
 }
@@ -856,7 +859,8 @@ static int launch(const occult_cfg_t& c, const Args& a, const Args* b, int group
   // 39.2; 8 rows 47.6 | 45.7 | 52.6; 16 rows 65.7 | 59.8 | 56.7; 23 rows 65.0 | 59.7 | 57.7; 46 rows 108 | 92 | 83; with groups
   // of 32, whose four scalings per block take registers, 23 rows 72.3 | 67.0 | 71.0, 46 rows 137 | 119 | 125.  Down product: 12 rows
   // 34.1 | 32.3 | 32.5; 16 rows 41.5 | 42.6 | 50.6; 23 rows 43.8 | 41.4 | 37.9; 46 rows 72 | 64 | 52.
-  if (per_expert >= (NW == 2 ? 16 : 20) && (NW == 1 || group != 32)) return launch_typed<true, 2, 2, NW, false, 1>(a, b, group, zeros, rows, s);
+  if (per_expert >= (NW == 2 ? 16 : 20) && (NW == 1 || group != 32))
+    return launch_typed<true, 2, 2, NW, false, 1, 0, 4, NW == 2 ? 64 : 32>(a, b, group, zeros, rows, s);
   if (per_expert >= 8) return launch_typed<true, 2, 1, NW, false, 1>(a, b, group, zeros, rows, s);
   return launch_typed<true, 1, 1, NW, false, 1>(a, b, group, zeros, rows, s);
 }
