@@ -250,6 +250,8 @@ class OccultLayer:
         w_down, or None for the 4-bit ones), and norm.forward(x, y, **params), a norm.BlockNorm that adds y to the residual stream x
         and norms it for the next block -> out, the next block's h.  Router scores stay in self.logits."""
         s = self.shape
+        if (norm.T, norm.d, norm.tdtype) != (s["T"], s["d"], self.tdtype):   # its calls see addresses: other rows of the same total
+            raise ValueError(f"occult: norm is for {norm.T} rows of {norm.d} {norm.tdtype}, the layer for {s['T']} of {s['d']} {self.tdtype}")
         self.route_from_hidden(h, w_router, self._buf("logits", (s["T"], s["E"]), torch.float32))
         self.make_plan()
         self.dispatch(h)
