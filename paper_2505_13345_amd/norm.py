@@ -59,8 +59,10 @@ class BlockNorm:
             return None
         if t.get_device() != self.device.index:
             raise ValueError(f"occult: {name} is on {t.device}, the buffers are on {self.device}")
-        B.expect(t, name, self.tdtype, numel)
-        return B._ptr(t)
+        if t.dtype != self.tdtype or t.numel() < numel or not t.is_contiguous():
+            B.expect(t, name, self.tdtype, numel)   # says what is wrong
+            B._ptr(t)
+        return t.data_ptr()
 
     def _describe(self, gate, post_weight, post_bias, pre_weight, pre_bias):
         if torch.cuda.current_device() != self.device.index:   # the library launches on the current device's stream
