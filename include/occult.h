@@ -261,7 +261,8 @@ int occult_expert_ffn_packed(const occult_cfg_t* cfg, const occult_plan_t* plan,
 /* 4-bit expert weights with group scales, for serving from a quarter of the memory (decoding streams the active experts' weights
  * once per step): weight k of a row of K is
  *   scale[k / group] * (code[k] - zero[k / group]),   code 0..15, group 32, 64 or 128 (a row's last group may be shorter),
- * scales bf16 in layers of either dtype, zero points 0..15 or, with zeros[] NULL, 8 everywhere.  Device ptrs, in the order gate, up, down;
+ * scales bf16 in layers of either dtype (scales kept in fp16 elsewhere are the caller's to round, which costs them three bits), zero
+ * points 0..15 or, with zeros[] NULL, 8 everywhere.  Device ptrs, in the order gate, up, down;
  * the rows are those of occult_weights_t:
  *   codes  [E+S][rows][K / 2]             two codes per byte, the lower k in the low bits; 16-byte aligned
  *   scales [E+S][rows][ceil(K / group)]   zeros [E+S][rows][ceil(K / group)]
@@ -271,15 +272,15 @@ int occult_expert_ffn_packed(const occult_cfg_t* cfg, const occult_plan_t* plan,
  *   zeros[] given of (max(w, 0) - min(w, 0)) / 15; zero = round(-min / scale); code = round(w / scale) + zero, clamped.
  *   A group of zeros gets scale 0 and codes 8.
  * occult_dequantize_weights writes the values they stand for in cfg.dtype, in the layout of occult_weights_t (rounded to nearest): for
- *   batches of more than about 130 rows per expert, where occult_expert_ffn on them is the faster way.
+ *   batches of more than about 130 rows per expert (with groups of 32, 60), where occult_expert_ffn on them is the faster way.
  * occult_pack_w4 writes codes and scales in the order the products read them (occult_pack_w4_bytes() bytes, 16-byte aligned; nothing
  *   else is read afterwards): per matrix (gate and up in pairs) units of 16 rows, per unit K blocks of 128, per block and
  *   matrix 64 pieces of 16 bytes, piece l = row l % 16, whose dword j holds K elements j * 32 + (l / 16) * 8 .. + 8: element 2i in bits
  *   4i .. 4i + 3, 2i + 1 in bits 16 + 4i .., rotated left by 3.  Scales follow the codes of all matrices in the same order.
  * occult_expert_ffn_w4 is occult_expert_ffn computed from them: same plan, same rows, same outputs; products of x and codes are
  *   summed in f32 per group and scaled in f32 (f32 layers: x is not rounded either; a row of x with an infinity or NaN gives
- *   non-finite rows, of either kind); h is rounded to cfg.dtype between the
- *   two products.  cfg.ffn_phase as there.  Which kernel computes a product, and with it the last bits, depends on T, E, k, S, d and
+ *   non-finite rows, of either kind; a group's sum before its scale may reach 31 * 128 * max|x|, so values of x beyond 2^115 may
+ *   overflow it); h is rounded to cfg.dtype between the two products.  cfg.ffn_phase as there.  Which kernel computes a product, and with it the last bits, depends on T, E, k, S, d and
  *   f; for one layer description results are the same bits every time.  A launch of 2^24 workgroups or more is refused (OCCULT_ESHAPE).
  * occult_forward_w4 is occult_forward with occult_expert_ffn_w4 in the place of the expert computation (no pre-activations
  *   are kept: buffers->epd_gu, gu_shared and ffn_ws are not used). */

@@ -9,9 +9,10 @@
 // Bound by HBM: a handful of operations per element.  Every row is read once and written once: the lanes that share a row keep it in
 // registers from the first sum to the last store, so the row statistics cost no second read, and the backward pass
 // recomputes them from the rows that it reads anyway instead of reading kept ones.  A row of up to 64 vectors of 16 bytes
-// belongs to the smallest power of two of lanes that holds it (a wave then works on several rows), a longer one to one wave with several
-// vectors per lane, and still longer ones to several waves, which exchange their sums through LDS.  All sums are f32; which lanes add
-// what depends on the row length alone, so a token's results do not depend on the batch around it.
+// belongs to the smallest power of two of lanes that holds it (a wave then works on several rows).  Longer rows, forward: two vectors
+// per lane, on one wave and beyond that on 2, 4, 8 or 16, which exchange their sums through LDS; backward, where the column sums
+// take registers: one vector per lane on 2, 3, 4, 5 or 8 waves, then two and four vectors on eight.  All sums are f32; which
+// lanes add what depends on the row length alone, so a token's results do not depend on the batch around it.
 #include "common.h"
 
 #include <math.h>
@@ -576,7 +577,7 @@ __global__ __launch_bounds__(1024) void column_sums_kernel(const ColumnArgs a) {
 // second wave (16384 rows of 2048 bf16: 47 us, with one 51, with four 51; one row 3.3, 2.8, 4.6).  Backward: one vector per lane up to eight
 // waves (the column sums take registers: 1000 rows of 2048 12.8 us, with two 15.8; 16384 rows the same 76, with
 // means and biases 92 against 126), then two and four (sixteen waves of two leave 128 registers: 2195 rows of 7640 f32 134 us, eight
-// of four 75; 2048 rows of 16384 bf16 299 and 209, both of which spill).
+// of four 75; 2048 rows of 16384 bf16 299 and 208, both of which spill, as do means and biases there: 320).
 struct Shape {
   int V, W, lanes;
 };

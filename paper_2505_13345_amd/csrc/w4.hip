@@ -258,7 +258,8 @@ __device__ __forceinline__ Place find_place(const Args& first, const Args& secon
 
 // The waves of a workgroup take equal parts of K of NB units of 16 output columns (NW matrices each: gate and up, or down) for up
 // to 16 rows of one group, and add their sums through LDS in the order of K.  For few rows, where the length of a wave's stream is
-// what counts; every wave has kRing - 1 K blocks in flight.
+// what counts; every wave has kRing - 1 K blocks in flight (gate/up, whose waves have four: one in flight, in fewer registers,
+// 10.6 us, three 12.7; 2 tokens, 64 experts and 2 shared).
 template <int NB, int NW, int G, bool ZERO, bool F32, int kRing, int WAVES>
 __device__ __forceinline__ void split_product(const Args& a, const TileInfo& ti, long long matrix, int unit0, float (*s_red)[NB * NW * 4][64]) {
   constexpr int kSteps = kBlockK / 32, kGroupSteps = kSteps / G;
@@ -850,6 +851,7 @@ static int launch(const occult_cfg_t& c, const Args& a, const Args* b, int group
     // A long sum over the shared experts' matrices beside short routed ones (K blocks: 44 of 4 shared experts, 22 of 2): 4 tokens split 12.2
     // against 24.3 us, 17 tokens 20.8 against 33.1, 64 tokens 27.7 against 38.4 (29.1 with codes three blocks ahead), 128 tokens 38.9
     // against 40.7 (36.2 with codes three blocks ahead).  With 2 shared, 4 tokens 11.1 against 13.7, 17 tokens 22.8 against 22.7.
+    // Nothing between 22 and 44 K blocks, or below 22, was measured: the borders at 20 and 32 stand for those two.
     const int chain = b ? b->mats * b->kblocks : 0;
     if ((chain >= 20 && chain >= c.T) || (chain >= 32 && c.T <= 64)) return launch_typed<true, 1, 1, 1, false, 1, 2>(a, b, group, zeros, rows, s);
     if (chain >= 32 && per_expert < 12) return launch_typed<true, 1, 1, 1, false, 4>(a, b, group, zeros, rows, s);

@@ -18,7 +18,8 @@ from . import binding as B
 class W4Weights(NamedTuple):
     """Expert weights in 4 bits, weight = scale * (code - zero), each field three tensors in the order gate, up, down:
     codes uint8 [E+S, rows, K / 2] (two along K per byte, the lower one in the low bits), scales bfloat16 and zeros uint8
-    [E+S, rows, ceil(K / group)]; zeros is None, or three Nones, where every zero point is 8."""
+    [E+S, rows, ceil(K / group)]; zeros is None, or three Nones, where every zero point is 8.  Scales of another type are the
+    caller's to round to bfloat16 (from float16 three bits of each are lost)."""
     group: int
     codes: tuple
     scales: tuple
