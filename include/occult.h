@@ -280,8 +280,9 @@ int occult_expert_ffn_packed(const occult_cfg_t* cfg, const occult_plan_t* plan,
  * occult_expert_ffn_w4 is occult_expert_ffn computed from them: same plan, same rows, same outputs; products of x and codes are
  *   summed in f32 per group and scaled in f32 (f32 layers: x is not rounded either; a row of x with an infinity or NaN gives
  *   non-finite rows, of either kind; a group's sum before its scale may reach 31 * 128 * max|x|, so values of x beyond 2^115 may
- *   overflow it); h is rounded to cfg.dtype between the two products.  cfg.ffn_phase as there.  Which kernel computes a product, and with it the last bits, depends on T, E, k, S, d and
- *   f; for one layer description results are the same bits every time.  A launch of 2^24 workgroups or more is refused (OCCULT_ESHAPE).
+ *   overflow it); h is rounded to cfg.dtype between the two products.  cfg.ffn_phase as there.  Which kernel computes a product, and
+ *   with it the last bits, depends on T, E, k, S, d, f and group; for one layer description and form of the weights results are the same
+ *   bits every time.  A launch of 2^24 workgroups or more is refused (OCCULT_ESHAPE).
  * occult_forward_w4 is occult_forward with occult_expert_ffn_w4 in the place of the expert computation (no pre-activations
  *   are kept: buffers->epd_gu, gu_shared and ffn_ws are not used). */
 typedef struct occult_w4_weights {

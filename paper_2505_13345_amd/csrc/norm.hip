@@ -768,8 +768,8 @@ extern "C" int occult_block_norm_backward(const occult_cfg_t* cfg, const occult_
   a.ws = static_cast<float*>(ws);
   a.T = c.T; a.row_vecs = c.d * elem_size(c) / 16;
   a.post = n->post_kind; a.pre = n->pre_kind; a.gate_kind = n->gate_kind; a.sums = sums;
-  // the pre norm alone: h = N_pre(x) has no x_scale in it
-  const bool alone = !y && !dy && n->post_kind == OCCULT_NORM_NONE && n->gate_kind == OCCULT_GATE_NONE;
+  // the pre norm alone: h = N_pre(x) has no x_scale in it (without a pre norm there is no such call, and a y was there)
+  const bool alone = !y && !dy && n->pre_kind && n->post_kind == OCCULT_NORM_NONE && n->gate_kind == OCCULT_GATE_NONE;
   a.x_scale = alone ? 1.0f : n->x_scale; a.y_scale = n->y_scale; a.post_eps = n->post_eps; a.pre_eps = n->pre_eps;
   a.offset = n->weight_offset; a.inv_d = 1.0f / (float)c.d;
   hipStream_t st = static_cast<hipStream_t>(stream);

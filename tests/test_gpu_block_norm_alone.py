@@ -54,3 +54,14 @@ def test_frozen_block_behind_a_post_norm_or_a_gate():
         got = torch.full_like(dx, 7.0)
         B.occult_block_norm_backward(norm.cfg, desc, None, out, t["dout"], t["dh"], got, None)
         assert torch.equal(got, dx), (post, gate)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_residual_sum_without_any_norm(dtype):
+    """out = x_scale * x + y_scale * y: without a pre norm there is no form without y, so x_scale is in dx whatever is handed over."""
+    norm, t, p, *_ = case(9, 264, dtype, None, None, None, seed=6)
+    out, _ = norm.forward(t["x"], t["y"])
+    ref = norm.backward(out, t["dout"], y=t["y"])["dx"].clone()
+    assert torch.equal(ref, (t["dout"].float() * 0.75).to(ref.dtype))
+    for kw in (dict(), dict(want_dy=False), dict(want_dy=True)):
+        assert torch.equal(norm.backward(out, t["dout"], **kw)["dx"], ref), kw
